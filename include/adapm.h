@@ -44,7 +44,8 @@ typedef enum {
   ADAPM_ESTATE = -4    /* call order / step number inconsistent */
 } adapm_status_t;
 
-typedef enum { ADAPM_F32 = 0, ADAPM_BF16 = 1 } adapm_dtype_t;
+/* ADAPM_E4M3 (8 bits, largest value 448) is an output type of adapm_norm_forward only. */
+typedef enum { ADAPM_F32 = 0, ADAPM_BF16 = 1, ADAPM_E4M3 = 2 } adapm_dtype_t;
 
 /* Momentum regime of a block (Sec. 4.1): none / full (eq. 5) / low-rank (Alg. 1). */
 typedef enum { ADAPM_MOM_NONE = 0, ADAPM_MOM_FULL = 1, ADAPM_MOM_LOWRANK = 2 } adapm_mom_t;
@@ -205,6 +206,102 @@ adapm_status_t adapm_profile_enable(adapm_ctx* ctx, int32_t on);
  * launches the number of launches.  Returns the number of entries. */
 int64_t adapm_profile_read(adapm_ctx* ctx, int64_t index, char* name, size_t name_cap, double* total_ms,
                            int64_t* launches);
+
+/* ---- The end of a model ---------------------------------------------------------------------------------------------
+ *
+ * What stands between the last layer and the gradients that adapm_step reads for the two blocks a table ends with, the
+ * final norm vector and the output head:
+ *
+ *     h = residual + dropout(x),   y = norm(h) * weight,   loss = cross entropy of y W^T,   and the way back.
+ *
+ * These calls need no context.  Like adapm_step they are asynchronous on the given stream of the CURRENT device,
+ * allocate nothing, never wait for the device and keep nothing between calls: they may be captured into a HIP graph, and
+ * calls on different streams may overlap if their outputs and workspaces differ.  Sums are held in fp32 or fp64 and added
+ * in a fixed order: the same inputs give the same bits.  rows = 0 is allowed everywhere. */
+
+/* A matrix of activations or weights: row r starts at data + r * stride elements (stride >= the row's length; any
+ * alignment to whole elements).  data = NULL: absent, where that is allowed. */
+typedef struct {
+  void* data;
+  int64_t stride;
+} adapm_rows_t;
+
+/* Dropout by a counter-based generator (Philox4x32-10): whether element (row, column) is kept depends on seed, offset, row and
+ * column alone, so the backward pass makes the same mask again and no mask is ever stored.  The probability is rounded
+ * to a multiple of 2^-16 (at most 65535 / 65536); what is kept is divided by one minus that.  What is dropped becomes 0
+ * whatever it was.  offset_dev (DEVICE, may be NULL) is added to offset: a captured graph whose replays have to draw new masks
+ * reads its counter there. */
+typedef struct {
+  uint64_t seed, offset;
+  const uint64_t* offset_dev;
+  float p;                         /* 0 <= p < 1 */
+  int32_t reserved;                /* 0 */
+} adapm_dropout_t;
+
+/* y = residual + dropout(x), rounded once; residual.data may be NULL.  The gradient of x is the same call on the gradient of
+ * y, without residual.  y may be x or residual. */
+adapm_status_t adapm_dropout(adapm_rows_t y, adapm_rows_t x, adapm_rows_t residual, int64_t rows, int64_t cols, int32_t dtype,
+                             const adapm_dropout_t* drop, void* stream);
+
+/* Root-mean-square norm with the residual's addition. */
+typedef struct {
+  int64_t rows, cols;              /* 1 <= cols <= 16384 */
+  int32_t dtype;                   /* x, residual, h and all gradients but dweight: F32 or BF16 */
+  int32_t weight_dtype;            /* F32 or BF16 */
+  int32_t y_dtype;                 /* forward: dtype, or ADAPM_E4M3 */
+  int32_t grad_dtype;              /* backward: dweight, F32 or BF16 */
+  float eps;
+  int32_t reserved;                /* 0 */
+} adapm_norm_t;
+
+/* h = residual + dropout(x) in dtype, rstd = 1 / sqrt(mean(h^2) + eps) (fp32, one a row), y = h * rstd * weight.
+ * residual.data and drop may be NULL; with neither, h.data may be NULL and the h of the backward pass is x itself.
+ * y_dtype = ADAPM_E4M3: y holds 8-bit values and y_scale[row] = max|row| / 448 (1 for a row of zeros; NaN does not count)
+ * is what they are multiplied by.  h may be x or residual; y overlaps none of the others. */
+adapm_status_t adapm_norm_forward(const adapm_norm_t* n, adapm_rows_t x, adapm_rows_t residual, adapm_rows_t h,
+                                  const void* weight_dev, adapm_rows_t y, float* y_scale_dev, float* rstd_dev,
+                                  const adapm_dropout_t* drop, void* stream);
+
+/* Scratch of adapm_norm_backward; 0 if n is invalid. */
+size_t adapm_norm_workspace_bytes(const adapm_norm_t* n);
+
+/* dy: gradient of y; dh: gradient of h from elsewhere, the residual stream (data may be NULL).  Writes dresidual (the gradient of
+ * h; data may be NULL), dx (dropout's factor times that) and dweight (cols values).  dx and dresidual may be dy or dh, but with
+ * dropout not one another; workspace_dev: adapm_norm_workspace_bytes() bytes, 256-byte aligned. */
+adapm_status_t adapm_norm_backward(const adapm_norm_t* n, adapm_rows_t dy, adapm_rows_t dh, adapm_rows_t h,
+                                   const void* weight_dev, const float* rstd_dev, adapm_rows_t dx, adapm_rows_t dresidual,
+                                   void* dweight_dev, const adapm_dropout_t* drop, void* workspace_dev, void* stream);
+
+/* loss = f * sum_i w_i (lse_i - s_i,target(i)), s = x W^T: softmax cross entropy over a vocabulary whose logits are never
+ * kept.  f = scale, divided by the number of rows that count with ADAPM_REDUCE_MEAN. */
+typedef enum { ADAPM_REDUCE_SUM = 0, ADAPM_REDUCE_MEAN = 1 } adapm_reduction_t;
+typedef struct {
+  int64_t rows, vocab, cols;       /* x: rows x cols; W: vocab x cols; rows <= 2^22, vocab <= 2^21, cols <= 2^16 */
+  int32_t dtype;                   /* x, W and their gradients: F32 or BF16 */
+  int32_t reduction;               /* adapm_reduction_t */
+  float scale;
+  int32_t reserved;                /* 0 */
+} adapm_head_t;
+
+/* Scratch of adapm_head_loss (backward = 0) or adapm_head_backward (1); 0 if h is invalid.  weight: as in the call (W whose rows
+ * are not whole, 16-byte aligned vectors is copied there). */
+size_t adapm_head_workspace_bytes(const adapm_head_t* h, adapm_rows_t weight, int32_t backward);
+
+/* targets[rows]: a row whose target lies outside [0, vocab) does not count: whatever it holds reaches nothing, its row_loss
+ * and lse are 0.  row_weight[rows] (may be NULL: 1).  Writes loss (one float), row_loss[rows] (not weighted) and lse[rows], which
+ * the backward pass needs.  If no row counts the loss is 0. */
+adapm_status_t adapm_head_loss(const adapm_head_t* h, adapm_rows_t x, adapm_rows_t weight, const int64_t* targets_dev,
+                               const float* row_weight_dev, float* loss_dev, float* row_loss_dev, float* lse_dev,
+                               void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Gradients of upstream * loss (upstream_dev: one float, NULL: 1) by x and W, for the same arguments and the lse of
+ * adapm_head_loss.  Either of dx and dweight may have data = NULL; rows that do not count get dx = 0.  All vocab rows of dweight
+ * are written: for the output head of a table that buffer is the block's gradient in adapm_step.  bf16: P = w (softmax - onehot) is
+ * rounded to bf16 between the products. */
+adapm_status_t adapm_head_backward(const adapm_head_t* h, adapm_rows_t x, adapm_rows_t weight, const int64_t* targets_dev,
+                                   const float* row_weight_dev, const float* lse_dev, const float* upstream_dev,
+                                   adapm_rows_t dx, adapm_rows_t dweight, void* workspace_dev, size_t workspace_bytes,
+                                   void* stream);
 
 const char* adapm_last_error(void);
 

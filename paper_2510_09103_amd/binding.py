@@ -18,10 +18,11 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libadapm.so")
 
 ADAPM_OK, ADAPM_EINVAL, ADAPM_ENOMEM, ADAPM_EHIP, ADAPM_ESTATE = 0, -1, -2, -3, -4
-ADAPM_F32, ADAPM_BF16 = 0, 1
+ADAPM_F32, ADAPM_BF16, ADAPM_E4M3 = 0, 1, 2
 ADAPM_MOM_NONE, ADAPM_MOM_FULL, ADAPM_MOM_LOWRANK = 0, 1, 2
 ADAPM_V_ELEMENT, ADAPM_V_ROWGROUP, ADAPM_V_WHOLE = 0, 1, 2
 ADAPM_CONTRACT_AUTO, ADAPM_CONTRACT_F64, ADAPM_CONTRACT_BF16X2 = 0, 1, 2
+ADAPM_REDUCE_SUM, ADAPM_REDUCE_MEAN = 0, 1
 
 
 class adapm_block_t(C.Structure):
@@ -40,12 +41,33 @@ class adapm_hparams_t(C.Structure):
                 ("seed", C.c_uint64)]
 
 
+class adapm_rows_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64)]
+
+
+class adapm_dropout_t(C.Structure):
+    _fields_ = [("seed", C.c_uint64), ("offset", C.c_uint64), ("offset_dev", C.c_void_p), ("p", C.c_float),
+                ("reserved", C.c_int32)]
+
+
+class adapm_norm_t(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("dtype", C.c_int32), ("weight_dtype", C.c_int32),
+                ("y_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
+class adapm_head_t(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("vocab", C.c_int64), ("cols", C.c_int64), ("dtype", C.c_int32),
+                ("reduction", C.c_int32), ("scale", C.c_float), ("reserved", C.c_int32)]
+
+
 EXPORTS = ["adapm_init", "adapm_state_bytes", "adapm_workspace_bytes", "adapm_state_offsets",
            "adapm_state_init", "adapm_state_loaded", "adapm_step", "adapm_block_contraction", "adapm_last_launch_count",
            "adapm_algorithmic_bytes",
            "adapm_algorithmic_flops", "adapm_profile_enable", "adapm_profile_read", "adapm_last_error",
            "adapm_set_grad_clip", "adapm_last_grad_norm", "adapm_lr_cosine_warmup", "adapm_destroy",
-           "adapm_step_static", "adapm_static_scratch_bytes"]
+           "adapm_step_static", "adapm_static_scratch_bytes",
+           "adapm_dropout", "adapm_norm_forward", "adapm_norm_workspace_bytes", "adapm_norm_backward",
+           "adapm_head_workspace_bytes", "adapm_head_loss", "adapm_head_backward"]
 
 
 def _load() -> C.CDLL:
@@ -94,6 +116,21 @@ def _load() -> C.CDLL:
                                        C.POINTER(C.c_int64)]
     lib.adapm_last_error.restype = C.c_char_p
     lib.adapm_last_error.argtypes = []
+    R, D, N, H = adapm_rows_t, C.POINTER(adapm_dropout_t), C.POINTER(adapm_norm_t), C.POINTER(adapm_head_t)
+    lib.adapm_dropout.restype = C.c_int
+    lib.adapm_dropout.argtypes = [R, R, R, C.c_int64, C.c_int64, C.c_int32, D, P]
+    lib.adapm_norm_forward.restype = C.c_int
+    lib.adapm_norm_forward.argtypes = [N, R, R, R, P, R, P, P, D, P]
+    lib.adapm_norm_workspace_bytes.restype = C.c_size_t
+    lib.adapm_norm_workspace_bytes.argtypes = [N]
+    lib.adapm_norm_backward.restype = C.c_int
+    lib.adapm_norm_backward.argtypes = [N, R, R, R, P, P, R, R, P, D, P, P]
+    lib.adapm_head_workspace_bytes.restype = C.c_size_t
+    lib.adapm_head_workspace_bytes.argtypes = [H, R, C.c_int32]
+    lib.adapm_head_loss.restype = C.c_int
+    lib.adapm_head_loss.argtypes = [H, R, R, P, P, P, P, P, P, C.c_size_t, P]
+    lib.adapm_head_backward.restype = C.c_int
+    lib.adapm_head_backward.argtypes = [H, R, R, P, P, P, P, R, R, P, C.c_size_t, P]
     lib.adapm_destroy.restype = None
     lib.adapm_destroy.argtypes = [P]
     return lib
@@ -214,6 +251,50 @@ def adapm_profile_read(ctx):
 
 def adapm_destroy(ctx):
     lib.adapm_destroy(ctx)
+
+
+# The end of a model.  Matrices are adapm_rows_t (rows() below), device pointers are integers, 0 for NULL.
+
+def rows(data: int = 0, stride: int = 0) -> adapm_rows_t:
+    return adapm_rows_t(data or None, stride)
+
+
+def _ref(s):
+    return None if s is None else C.byref(s)
+
+
+def adapm_dropout(y, x, residual, n_rows: int, cols: int, dtype: int, drop, stream: int = 0):
+    _check(lib.adapm_dropout(y, x, residual, n_rows, cols, dtype, _ref(drop), stream))
+
+
+def adapm_norm_forward(n, x, residual, h, weight_ptr: int, y, y_scale_ptr: int, rstd_ptr: int, drop=None, stream: int = 0):
+    _check(lib.adapm_norm_forward(_ref(n), x, residual, h, weight_ptr, y, y_scale_ptr, rstd_ptr, _ref(drop), stream))
+
+
+def adapm_norm_workspace_bytes(n) -> int:
+    return lib.adapm_norm_workspace_bytes(_ref(n))
+
+
+def adapm_norm_backward(n, dy, dh, h, weight_ptr: int, rstd_ptr: int, dx, dresidual, dweight_ptr: int, drop, workspace_ptr: int,
+                        stream: int = 0):
+    _check(lib.adapm_norm_backward(_ref(n), dy, dh, h, weight_ptr, rstd_ptr, dx, dresidual, dweight_ptr, _ref(drop), workspace_ptr,
+                                   stream))
+
+
+def adapm_head_workspace_bytes(h, weight, backward: bool) -> int:
+    return lib.adapm_head_workspace_bytes(_ref(h), weight, 1 if backward else 0)
+
+
+def adapm_head_loss(h, x, weight, targets_ptr: int, row_weight_ptr: int, loss_ptr: int, row_loss_ptr: int, lse_ptr: int,
+                    workspace_ptr: int, workspace_bytes: int, stream: int = 0):
+    _check(lib.adapm_head_loss(_ref(h), x, weight, targets_ptr, row_weight_ptr, loss_ptr, row_loss_ptr, lse_ptr, workspace_ptr,
+                               workspace_bytes, stream))
+
+
+def adapm_head_backward(h, x, weight, targets_ptr: int, row_weight_ptr: int, lse_ptr: int, upstream_ptr: int, dx, dweight,
+                        workspace_ptr: int, workspace_bytes: int, stream: int = 0):
+    _check(lib.adapm_head_backward(_ref(h), x, weight, targets_ptr, row_weight_ptr, lse_ptr, upstream_ptr, dx, dweight, workspace_ptr,
+                                   workspace_bytes, stream))
 
 
 def ptr_array(ptrs: Sequence[int]):

@@ -7,6 +7,7 @@
 // the update on the host.
 #include "../../include/adapm.h"
 #include "adapm_plan.h"
+#include "ops_plan.h"
 
 #include <algorithm>
 #include <cmath>
@@ -21,10 +22,9 @@
 
 using namespace adapm;
 
-namespace {
+static thread_local std::string g_err;
 
-thread_local std::string g_err;
-
+namespace adapm {
 adapm_status_t fail(adapm_status_t code, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -34,6 +34,9 @@ adapm_status_t fail(adapm_status_t code, const char* fmt, ...) {
   g_err = buf;
   return code;
 }
+}  // namespace adapm
+
+namespace {
 
 #define HIP_TRY(expr)                                                                      \
   do {                                                                                     \

@@ -1,0 +1,741 @@
+// Softmax cross entropy of logits s = x W^T that are never kept, and its gradient.
+//
+//   forward   lse_i = log sum_v exp s_iv,  loss_i = lse_i - s_i,t_i
+//   backward  P = w_i (exp(s - lse) - onehot),  dx = f P W,  dW = f P^T x      (f: reduction, scale, upstream gradient)
+//
+// Forward: a workgroup makes one tile of logits on the matrix cores and leaves only the maximum and the sum of exponentials of its
+// columns for every row; a second launch joins them.  Backward: the vocabulary is taken in pieces; for each, P is made from fresh
+// logits and stored in the type of x (a piece is at most PIECE_BYTES, not the rows x vocab of all logits), then one launch adds
+// its part to dx and writes its rows of dW.  The logits are made twice because keeping them does not pay here: at 1600 columns a
+// logit costs 3.2 kflop, 3 ps of the matrix cores at the rate these kernels reach; to write it in fp32, read it and write P again
+// takes 10 bytes, 2 ps of memory, and as much memory as the operator is there to save.
+//
+// Rows without a target are left out before anything else: the rows that count are packed side by side (padded to whole steps of the
+// contraction), so masked rows cost nothing, and whatever stands in them (NaN included) reaches no sum.
+#include "ew_math.h"
+#include "ops_plan.h"
+
+namespace adapm {
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef u32x2 u32x2_e2 __attribute__((aligned(2), may_alias));
+typedef f32x4 f32x4_e4 __attribute__((aligned(4), may_alias));
+typedef __attribute__((address_space(3))) unsigned char lds_u8;
+
+constexpr unsigned OOB = 0x80000000u;                 // an offset past every descriptor's end: reads zeros
+constexpr int64_t PIECE_BYTES = (int64_t)128 << 20;   // most of P at a time: half of what the last-level cache holds
+constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LN2 = 0.69314718055994530942f;
+
+struct HeadHeader {
+  int n;                                              // rows that count
+  int pad[63];
+};
+
+__device__ __forceinline__ float grad_factor(const HeadDev& h, int n) {
+  float f = h.scale * (h.upstream ? *h.upstream : 1.f);
+  return h.mean ? f / (float)(n > 0 ? n : 1) : f;
+}
+
+// ---- rows that count -------------------------------------------------------------------------------------------------
+constexpr int COUNT_ROWS = 1024;                      // rows of a workgroup of the count, and of an entry of its result
+constexpr int PACK_ROWS = 16;                         // rows of a workgroup of the packing
+
+__device__ __forceinline__ bool counts(const HeadDev& h, int64_t row) {
+  const int64_t t = h.targets[row];
+  return t >= 0 && t < h.vocab;
+}
+
+__global__ __launch_bounds__(256) void count_kernel(HeadDev h) {
+  __shared__ int red[4];
+  int c = 0;
+  for (int i = threadIdx.x; i < COUNT_ROWS; i += 256) {
+    const int64_t row = (int64_t)blockIdx.x * COUNT_ROWS + i;
+    c += row < h.rows && counts(h, row) ? 1 : 0;
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) c += __shfl_xor(c, o);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
+  __syncthreads();
+  if (threadIdx.x == 0) reinterpret_cast<int*>(h.ws + h.lay.counts)[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+}
+
+// Places of the rows that count (in their order) and their packed copies.  A workgroup finds how many stand before its own from
+// the counts of the thousands before and from the targets of its own thousand.
+template <class T>
+__global__ __launch_bounds__(256) void pack_kernel(HeadDev h) {
+  __shared__ int red[4];
+  __shared__ int place[PACK_ROWS];
+  const int64_t r0 = (int64_t)blockIdx.x * PACK_ROWS;
+  const int64_t b0 = r0 / COUNT_ROWS;
+  int c = 0;
+  const int* counted = reinterpret_cast<const int*>(h.ws + h.lay.counts);
+  for (int64_t i = threadIdx.x; i < b0; i += 256) c += counted[i];
+  for (int64_t row = b0 * COUNT_ROWS + threadIdx.x; row < r0; row += 256) c += counts(h, row) ? 1 : 0;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) c += __shfl_xor(c, o);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const int64_t row = r0 + threadIdx.x;
+    const bool in = threadIdx.x < PACK_ROWS && row < h.rows;
+    const bool live = in && counts(h, row);
+    const unsigned long long m = __ballot(live);
+    const int before = red[0] + red[1] + red[2] + red[3];
+    const int j = before + __popcll(m & ((1ull << threadIdx.x) - 1));
+    if (in) {
+      place[threadIdx.x] = live ? j : -1;
+      reinterpret_cast<int*>(h.ws + h.lay.place)[row] = live ? j : -1;
+      if (live) {
+        reinterpret_cast<int*>(h.ws + h.lay.list)[j] = (int)row;
+        reinterpret_cast<int*>(h.ws + h.lay.target)[j] = (int)h.targets[row];
+        reinterpret_cast<float*>(h.ws + h.lay.weight)[j] = h.row_weight ? h.row_weight[row] : 1.f;
+        if (!h.row_loss) reinterpret_cast<float*>(h.ws + h.lay.lse)[j] = h.lse[row];       // backward
+      } else if (h.row_loss) {
+        h.row_loss[row] = 0.f;
+        h.lse[row] = 0.f;
+      }
+    }
+    if (threadIdx.x == 0 && r0 + PACK_ROWS >= h.rows) reinterpret_cast<HeadHeader*>(h.ws + h.lay.head)->n = before + __popcll(m);
+  }
+  __syncthreads();
+  T* out = reinterpret_cast<T*>(h.ws + h.lay.x);
+  const T* x = reinterpret_cast<const T*>(h.x.p);
+  for (int i = 0; i < PACK_ROWS; ++i) {
+    if (r0 + i >= h.rows || place[i] < 0) continue;
+    for (int c2 = threadIdx.x; c2 < h.pitch; c2 += 256)
+      out[(int64_t)place[i] * h.pitch + c2] = c2 < h.cols ? x[(r0 + i) * h.x.stride + c2] : T(0);
+  }
+}
+
+// W with rows that are no whole, aligned vectors
+template <class T>
+__global__ __launch_bounds__(256) void pack_w_kernel(HeadDev h) {
+  T* out = reinterpret_cast<T*>(h.ws + h.lay.w) + (int64_t)blockIdx.x * h.pitch;
+  const T* w = reinterpret_cast<const T*>(h.w.p) + (int64_t)blockIdx.x * h.w.stride;
+  for (int c = threadIdx.x; c < h.pitch; c += 256) out[c] = c < h.cols ? w[c] : T(0);
+}
+
+// ---- matrix products -------------------------------------------------------------------------------------------------
+// A tile of D[m][n] = sum_k A(m, k) B(n, k).  An operand is stored with k along its rows (KC: element (u, k) at u pitch + k) or
+// across them (at k pitch + u).  128-byte slices of the contraction (64 bf16 or 32 fp32 values) go through two LDS buffers: the
+// next slice is loaded into registers while the current one feeds the matrix cores.  Pieces of 16 bytes are exchanged within an LDS
+// row (by the row's number) so that the reads of a fragment fall on different banks without padding.
+// bf16: v_mfma_f32_16x16x32, KC fragments are one 16-byte read, the others two transposing reads of 8 bytes.
+// fp32: v_mfma_f32_16x16x4, four of them to a 16-byte read; which k meets which instruction is the same for both operands.
+struct Src {
+  const char* p;        // element (0, 0)
+  int64_t pitch;        // bytes
+  int u, k;             // extent of the free index and of the contraction, in elements
+};
+
+template <class T, int BU, int NTHR, bool KC>
+struct Operand {
+  static constexpr int ES = sizeof(T);
+  static constexpr int BK = 128 / ES;                 // elements of the contraction in a slice
+  static constexpr int BYTES = BU * 128;
+  static constexpr int NL = BYTES / (16 * NTHR);      // 16-byte pieces of a thread
+  static constexpr int RPC = BU * ES / 16;            // pieces of a row where k goes across
+  static_assert(NL * 16 * NTHR == BYTES, "whole pieces");
+
+  u32x4 r[NL];
+
+  __device__ __forceinline__ void load(const Src& s, int u0, int k0) {
+    const int tid = threadIdx.x;
+    if (KC) {
+      const int rows = s.u - u0 < BU ? s.u - u0 : BU;
+      const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(s.p + (int64_t)u0 * s.pitch), 0, (int)(rows * s.pitch), 0x00020000);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int c = tid + NTHR * i, row = c >> 3, ck = c & 7, k = k0 + ck * (16 / ES);
+        r[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, k < s.k ? (int)(row * s.pitch) + k * ES : (int)OOB, 0, 0);
+      }
+    } else {
+      const int rows = s.k - k0 < BK ? s.k - k0 : BK;
+      const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(s.p + (int64_t)k0 * s.pitch), 0, (int)(rows * s.pitch), 0x00020000);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int c = tid + NTHR * i, row = c / RPC, u = u0 + (c % RPC) * (16 / ES);
+        r[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, u < s.u ? (int)(row * s.pitch) + u * ES : (int)OOB, 0, 0);
+      }
+    }
+  }
+
+  // Where a piece goes.  KC: its place among the eight of its row is exchanged by the row's number.  Else pieces of 32 bytes (bf16; a
+  // read touches rows 0 .. 3 and 8 .. 11 of a step at a time) or 64 bytes (fp32; rows 0, 4, 8 and 12) are exchanged by the row, over the
+  // 256 bytes of all banks: where an LDS row is 128 bytes, its number's lowest bit says which half it lies in already.
+  static_assert(KC || (ES == 2 && BU * ES == 128) || BU * ES >= 256, "exchanged inside a row");
+  static __device__ __forceinline__ int swz(int k) {
+    if (ES == 4) return (k >> 2) & 3;
+    return BU * ES == 128 ? ((k >> 1) & 1) | ((k >> 2) & 2) : (k & 3) | ((k >> 1) & 4);
+  }
+
+  __device__ __forceinline__ void store(lds_u8* lds) const {
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int c = tid + NTHR * i;
+      int at;
+      if (KC) {
+        const int row = c >> 3, ck = c & 7;
+        at = row * 128 + ((ck ^ (row & 7)) << 4);
+      } else {
+        const int row = c / RPC, cu = c % RPC;
+        at = ES == 2 ? row * (BU * ES) + ((((cu >> 1) ^ swz(row)) << 1 | (cu & 1)) << 4)
+                     : row * (BU * ES) + ((((cu >> 2) ^ swz(row)) << 2 | (cu & 3)) << 4);
+      }
+      *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(lds + at) = r[i];
+    }
+  }
+};
+
+// fragment of 16 rows u .. u + 15: eight (bf16) or four (fp32) values of the contraction of step ks for this lane
+template <class T, int BU, bool KC>
+__device__ __forceinline__ u32x4 fragment(const lds_u8* lds, int u, int ks) {
+  constexpr int ES = sizeof(T);
+  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
+  if (KC) {
+    const int row = u + l16, ck = ks * 4 + q;
+    return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(lds + row * 128 + ((ck ^ (row & 7)) << 4));
+  }
+  union {
+    s16x4 h[2];
+    float f[4];
+    u32x4 v;
+  } r;
+  if (ES == 2) {
+    // lane s of a block of 16 points at row s / 4, columns 4 (s % 4) .. + 3 of a 4 x 16 tile; lane i receives column i of the four rows
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int k = ks * 32 + q * 8 + h * 4 + (l16 >> 2), c = u + (l16 & 3) * 4;
+      const int at = k * (BU * ES) + (((c >> 4) ^ Operand<T, BU, 64, KC>::swz(k)) << 5) + ((c & 15) << 1);
+      r.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds + at));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int k = ks * 16 + q * 4 + j, c = u + l16;
+      const int at = k * (BU * ES) + (((c >> 4) ^ Operand<T, BU, 64, KC>::swz(k)) << 6) + ((c & 15) << 2);
+      r.f[j] = *reinterpret_cast<const __attribute__((address_space(3))) float*>(lds + at);
+    }
+  }
+  return r.v;
+}
+
+__device__ __forceinline__ f32x4 mma(const u32x4& a, const u32x4& b, f32x4 c, const uint16_t*) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(const u32x4& a, const u32x4& b, f32x4 c, const float*) {
+  const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+  return c;
+}
+
+// waves WM x WN, each MT x NT tiles of 16 x 16
+template <class T_, int MT_, int NT_, int WM_, int WN_>
+struct Cfg {
+  typedef T_ T;
+  static constexpr int MT = MT_, NT = NT_, WM = WM_, WN = WN_;
+  static constexpr int BM = 16 * MT * WM, BN = 16 * NT * WN, THREADS = 64 * WM * WN;
+  static constexpr int LDS = 2 * (BM + BN) * 128;
+};
+
+template <class C>
+struct Acc {
+  f32x4 v[C::MT][C::NT];
+};
+
+// acc = the tile at (m0, n0), contraction over [k0, k1)
+template <class C, bool AKC, bool BKC>
+__device__ __forceinline__ void product(const Src& A, const Src& B, int m0, int n0, int k0, int k1, lds_u8* lds, Acc<C>& acc) {
+  typedef typename C::T T;
+  typedef Operand<T, C::BM, C::THREADS, AKC> OA;
+  typedef Operand<T, C::BN, C::THREADS, BKC> OB;
+  constexpr int HALF = OA::BYTES + OB::BYTES;
+  const int wave = threadIdx.x >> 6, um = (wave % C::WM) * 16 * C::MT, un = (wave / C::WM) * 16 * C::NT;
+#pragma unroll
+  for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+    for (int j = 0; j < C::NT; ++j) acc.v[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (k0 >= k1) return;
+  OA a;
+  OB b;
+  a.load(A, m0, k0);
+  b.load(B, n0, k0);
+  __syncthreads();                       // the buffers' last readers
+  a.store(lds);
+  b.store(lds + OA::BYTES);
+  __syncthreads();
+  int buf = 0;
+  for (int k = k0; k < k1; k += OA::BK) {
+    const bool more = k + OA::BK < k1;
+    if (more) {
+      a.load(A, m0, k + OA::BK);
+      b.load(B, n0, k + OA::BK);
+    }
+    const lds_u8* la = lds + buf * HALF;
+    const lds_u8* lb = la + OA::BYTES;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      u32x4 fa[C::MT], fb[C::NT];
+#pragma unroll
+      for (int j = 0; j < C::NT; ++j) fb[j] = fragment<T, C::BN, BKC>(lb, un + 16 * j, ks);
+#pragma unroll
+      for (int i = 0; i < C::MT; ++i) fa[i] = fragment<T, C::BM, AKC>(la, um + 16 * i, ks);
+#pragma unroll
+      for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+        for (int j = 0; j < C::NT; ++j) acc.v[i][j] = mma(fa[i], fb[j], acc.v[i][j], (const T*)nullptr);
+    }
+    buf ^= 1;
+    if (more) {
+      a.store(lds + buf * HALF);
+      b.store(lds + buf * HALF + OA::BYTES);
+    }
+    __syncthreads();
+  }
+}
+
+// Order of the tiles of a launch: workgroup i runs on XCD i mod 8, which gets a run of neighbouring tiles, eight along n for each
+// along m, so that the tiles that an XCD works on at a time share operands in its L2.  The grid is for all rows, the tiles in use are
+// those of the rows that count.
+__device__ __forceinline__ void place_tile(int id, int mt, int nt, int& m, int& n) {
+  const int total = mt * nt, x = id & 7, per = total >> 3, rest = total & 7;
+  const int l = x * per + (x < rest ? x : rest) + (id >> 3);
+  const int group = l / (8 * mt), first = group * 8, width = nt - first < 8 ? nt - first : 8, in = l - first * mt;
+  n = first + in % width;
+  m = in / width;
+}
+
+// element (i, j, e) of a wave's accumulators: m = 16 i + 4 (lane / 16) + e, n = 16 j + lane % 16
+#define HEAD_LANE                                                                                      \
+  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;          \
+  const int um = (wave % C::WM) * 16 * C::MT, un = (wave / C::WM) * 16 * C::NT;
+
+template <class T>
+__device__ __forceinline__ Src packed_x(const HeadDev& h, int n) {
+  return Src{h.ws + h.lay.x, (int64_t)h.pitch * (int)sizeof(T), n, h.pitch};
+}
+template <class T>
+__device__ __forceinline__ Src vocab_rows(const HeadDev& h, int64_t first, int64_t rows) {     // rows of W from `first`, k along them
+  if (h.w_packed) return Src{h.ws + h.lay.w + first * h.pitch * (int)sizeof(T), (int64_t)h.pitch * (int)sizeof(T), (int)rows, h.pitch};
+  return Src{reinterpret_cast<const char*>(h.w.p) + first * h.w.stride * (int)sizeof(T), h.w.stride * (int)sizeof(T), (int)rows, h.cols};
+}
+
+// forward: m = vocabulary, n = rows of x
+template <class C>
+__global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_kernel(HeadDev h, int mt) {
+  typedef typename C::T T;
+  __shared__ __attribute__((aligned(128))) unsigned char smem[C::LDS];
+  const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
+  const int nt = (n + C::BN - 1) / C::BN;
+  if ((int)blockIdx.x >= mt * nt) return;
+  int tm, tn;
+  place_tile(blockIdx.x, mt, nt, tm, tn);
+  const int m0 = tm * C::BM, n0 = tn * C::BN;
+  Acc<C> acc;
+  product<C, true, true>(vocab_rows<T>(h, 0, h.vocab), packed_x<T>(h, n), m0, n0, 0, h.cols, (lds_u8*)smem, acc);
+  HEAD_LANE
+  const int* target = reinterpret_cast<const int*>(h.ws + h.lay.target);
+  float2* part = reinterpret_cast<float2*>(h.ws + h.lay.part) + (int64_t)(tm * C::WM + wave % C::WM) * h.rows;
+  float* hit = reinterpret_cast<float*>(h.ws + h.lay.hit);
+  const int v0 = m0 + um + 4 * q;
+#pragma unroll
+  for (int j = 0; j < C::NT; ++j) {
+    const int row = n0 + un + 16 * j + l16;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v0 + 16 * i + e < h.vocab) top = fmaxf(top, acc.v[i][j][e]);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    // a wave without a column of the vocabulary leaves (-inf, 0)
+    const float shift = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v0 + 16 * i + e < h.vocab) sum += __builtin_amdgcn_exp2f((acc.v[i][j][e] - shift) * LOG2E);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (row < n) {
+      if (q == 0) part[row] = make_float2(top, sum);
+      const int rel = target[row] - v0;
+      if (rel >= 0 && rel < 16 * C::MT && (rel & 15) < 4) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s = rel == 16 * i + e ? acc.v[i][j][e] : s;
+        hit[row] = s;
+      }
+    }
+  }
+}
+
+// joins the tiles' maxima and sums of 64 rows: 16 wavefronts share the tiles; each row's loss, and the workgroup's sum of them
+__global__ __launch_bounds__(1024) void finish_kernel(HeadDev h, int tiles, int last) {
+  __shared__ float rm[16][64], rs[16][64];
+  const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, row = blockIdx.x * 64 + l;
+  const float2* part = reinterpret_cast<const float2*>(h.ws + h.lay.part);
+  double* sums = reinterpret_cast<double*>(h.ws + h.lay.sums);
+  float m = -INFINITY, s = 0.f;
+  if (row < n)
+    for (int t = w; t < tiles; t += 16) {
+      const float2 p = part[(int64_t)t * h.rows + row];
+      if (p.y == 0.f) continue;                        // a tile behind the vocabulary's end
+      const float top = fmaxf(m, p.x);
+      s = (s == 0.f ? 0.f : s * __builtin_amdgcn_exp2f((m - top) * LOG2E)) + p.y * __builtin_amdgcn_exp2f((p.x - top) * LOG2E);
+      m = top;
+    }
+  rm[w][l] = m;
+  rs[w][l] = s;
+  __syncthreads();
+  if (w) return;
+  double part_loss = 0.0;
+  if (row < n) {
+    float top = rm[0][l];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, rm[i][l]);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (rs[i][l] != 0.f) sum += rs[i][l] * __builtin_amdgcn_exp2f((rm[i][l] - top) * LOG2E);
+    // the difference of the logits first, which is exact where they are near: a small loss keeps its digits
+    const float log_sum = logf(sum), lse = top + log_sum, loss = (top - reinterpret_cast<const float*>(h.ws + h.lay.hit)[row]) + log_sum;
+    const int to = reinterpret_cast<const int*>(h.ws + h.lay.list)[row];
+    h.lse[to] = lse;
+    h.row_loss[to] = loss;
+    part_loss = (double)reinterpret_cast<const float*>(h.ws + h.lay.weight)[row] * (double)loss;
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) part_loss += __shfl_xor(part_loss, o);
+  if (l) return;
+  if (last) *h.loss = (float)(part_loss * (double)h.scale / (h.mean ? (double)(n > 0 ? n : 1) : 1.0));
+  else sums[blockIdx.x] = part_loss;
+}
+
+__global__ __launch_bounds__(256) void total_kernel(HeadDev h, int groups) {
+  __shared__ double red[256];
+  const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
+  const double* sums = reinterpret_cast<const double*>(h.ws + h.lay.sums);
+  double s = 0.0;
+  for (int i = threadIdx.x; i < groups; i += 256) s += sums[i];
+  red[threadIdx.x] = s;
+  __syncthreads();
+  for (int o = 128; o > 0; o >>= 1) {
+    if ((int)threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *h.loss = (float)(red[0] * (double)h.scale / (h.mean ? (double)(n > 0 ? n : 1) : 1.0));
+}
+
+// a batch without rows: loss 0, dW 0
+__global__ __launch_bounds__(64) void no_rows_loss_kernel(HeadDev h) { *h.loss = 0.f; }
+
+template <class T>
+__global__ __launch_bounds__(256) void no_rows_dw_kernel(HeadDev h) {
+  T* to = reinterpret_cast<T*>(h.dw.p) + (int64_t)blockIdx.x * h.dw.stride;
+  for (int c = threadIdx.x; c < h.cols; c += 256) to[c] = T(0);
+}
+
+// backward: P of the vocabulary rows [first, first + width), m = vocabulary, n = rows of x; zeros up to the piece's pitch
+template <class C>
+__global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void piece_kernel(HeadDev h, int64_t first, int width, int64_t pitch, int mt) {
+  typedef typename C::T T;
+  __shared__ __attribute__((aligned(128))) unsigned char smem[C::LDS];
+  const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
+  const int nt = (n + C::BN - 1) / C::BN;
+  if ((int)blockIdx.x >= mt * nt) return;
+  int tm, tn;
+  place_tile(blockIdx.x, mt, nt, tm, tn);
+  const int m0 = tm * C::BM, n0 = tn * C::BN;
+  Acc<C> acc;
+  product<C, true, true>(vocab_rows<T>(h, first, width), packed_x<T>(h, n), m0, n0, 0, h.cols, (lds_u8*)smem, acc);
+  HEAD_LANE
+  T* P = reinterpret_cast<T*>(h.ws + h.lay.p);
+#pragma unroll
+  for (int j = 0; j < C::NT; ++j) {
+    const int row = n0 + un + 16 * j + l16;
+    if (row >= n) continue;
+    const int target = reinterpret_cast<const int*>(h.ws + h.lay.target)[row] - (int)first;
+    const float weight = reinterpret_cast<const float*>(h.ws + h.lay.weight)[row];
+    const float lse = reinterpret_cast<const float*>(h.ws + h.lay.lse)[row];
+#pragma unroll
+    for (int i = 0; i < C::MT; ++i) {
+      const int v = m0 + um + 16 * i + 4 * q;
+      float p[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        // fp32: the accurate exponential; bf16 rounds P to 8 bits (the matrix cores' operand), the hardware's is far inside that
+        const float x = sizeof(T) == 4 ? expf(acc.v[i][j][e] - lse) : __builtin_amdgcn_exp2f((acc.v[i][j][e] - lse) * LOG2E);
+        p[e] = v + e < width ? weight * (x - (v + e == target ? 1.f : 0.f)) : 0.f;
+      }
+      T* to = P + (int64_t)row * pitch + v;
+      if (v < pitch) {
+        if (sizeof(T) == 2) {
+          u32x2 w;
+          w[0] = pack_bf16x2(p[0], p[1]);
+          w[1] = pack_bf16x2(p[2], p[3]);
+          *reinterpret_cast<u32x2*>(to) = w;
+        } else {
+          *reinterpret_cast<f32x4*>(to) = f32x4{p[0], p[1], p[2], p[3]};
+        }
+      }
+    }
+  }
+}
+
+struct GradPlan {
+  int64_t first;          // the piece: vocabulary rows [first, first + width), P's row pitch in elements
+  int width;
+  int64_t pitch;
+  int mt;                 // tiles along the columns (both products)
+  int splits, k_split;    // dx: parts of the contraction and their length
+  int nt_w;               // dW: tiles along the vocabulary
+  int begin;              // first piece: dx's sums are written, not added to
+};
+
+// backward of a piece: workgroups [0, mt nt_w) make dW (m = columns, n = vocabulary, k = rows of x), the others dx (m = columns, n =
+// rows of x, k = the piece's vocabulary)
+template <class C>
+__global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_kernel(HeadDev h, GradPlan g) {
+  typedef typename C::T T;
+  __shared__ __attribute__((aligned(128))) unsigned char smem[C::LDS];
+  const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
+  const char* P = h.ws + h.lay.p;
+  const int64_t pp = g.pitch * (int64_t)sizeof(T);
+  const int n_dw = g.mt * g.nt_w;
+  HEAD_LANE
+  Acc<C> acc;
+  if ((int)blockIdx.x < n_dw) {
+    int tm, tn;
+    place_tile(blockIdx.x, g.mt, g.nt_w, tm, tn);
+    const int m0 = tm * C::BM, n0 = tn * C::BN;
+    product<C, false, false>(Src{h.ws + h.lay.x, (int64_t)h.pitch * (int)sizeof(T), h.pitch, n}, Src{P, pp, (int)g.pitch, n}, m0, n0, 0, n,
+                             (lds_u8*)smem, acc);
+    const float f = grad_factor(h, n);
+#pragma unroll
+    for (int j = 0; j < C::NT; ++j) {
+      const int v = n0 + un + 16 * j + l16;
+      if (v >= g.width) continue;
+      T* to = reinterpret_cast<T*>(h.dw.p) + (g.first + v) * h.dw.stride;
+#pragma unroll
+      for (int i = 0; i < C::MT; ++i) {
+        const int c = m0 + um + 16 * i + 4 * q;
+        const f32x4 x = acc.v[i][j] * f;
+        if (c + 4 <= h.cols) {
+          if (sizeof(T) == 2) {
+            u32x2 w;
+            w[0] = pack_bf16x2(x[0], x[1]);
+            w[1] = pack_bf16x2(x[2], x[3]);
+            *reinterpret_cast<u32x2_e2*>(to + c) = w;
+          } else {
+            *reinterpret_cast<f32x4_e4*>(to + c) = x;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (c + e < h.cols) to[c + e] = sizeof(T) == 2 ? (T)pack_bf16x2(x[e], 0.f) : (T)x[e];
+        }
+      }
+    }
+    return;
+  }
+  const int nt = (n + C::BN - 1) / C::BN, per = g.mt * nt, id = (int)blockIdx.x - n_dw;
+  if (id >= per * g.splits) return;
+  const int split = id / per;
+  int tm, tn;
+  place_tile(id - split * per, g.mt, nt, tm, tn);
+  const int m0 = tm * C::BM, n0 = tn * C::BN;
+  const int k0 = split * g.k_split, k1 = k0 + g.k_split < g.width ? k0 + g.k_split : g.width;
+  Src W = vocab_rows<T>(h, g.first, g.width);          // k across the rows
+  const int cols = W.k;
+  W.u = cols;
+  W.k = g.width;
+  product<C, false, true>(W, Src{P, pp, n, (int)g.pitch}, m0, n0, k0, k1, (lds_u8*)smem, acc);
+  float* sum = reinterpret_cast<float*>(h.ws + h.lay.acc) + (int64_t)split * h.rows * h.pitch;
+#pragma unroll
+  for (int j = 0; j < C::NT; ++j) {
+    const int row = n0 + un + 16 * j + l16;
+    if (row >= n) continue;
+#pragma unroll
+    for (int i = 0; i < C::MT; ++i) {
+      const int c = m0 + um + 16 * i + 4 * q;
+      if (c < h.pitch) {
+        f32x4* to = reinterpret_cast<f32x4*>(sum + (int64_t)row * h.pitch + c);
+        *to = g.begin ? acc.v[i][j] : *to + acc.v[i][j];
+      }
+    }
+  }
+}
+
+// dx of every row of x: the parts of its sum added in order, zeros where the row does not count
+template <class T>
+__global__ __launch_bounds__(256) void dx_kernel(HeadDev h, int splits) {
+  const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
+  const int64_t row = blockIdx.x;
+  const int j = reinterpret_cast<const int*>(h.ws + h.lay.place)[row];
+  const float* sum = reinterpret_cast<const float*>(h.ws + h.lay.acc);
+  const float f = grad_factor(h, n);
+  T* to = reinterpret_cast<T*>(h.dx.p) + row * h.dx.stride;
+  for (int c = threadIdx.x; c < h.cols; c += 256) {
+    float x = 0.f;
+    if (j >= 0)
+      for (int s = 0; s < splits; ++s) x += sum[((int64_t)s * h.rows + j) * h.pitch + c];
+    x *= f;
+    to[c] = sizeof(T) == 2 ? (T)pack_bf16x2(x, 0.f) : (T)x;
+  }
+}
+
+// ---- plans ------------------------------------------------------------------------------------------------------------
+typedef Cfg<uint16_t, 8, 4, 2, 4> Big;        // 256 x 256, eight wavefronts
+typedef Cfg<uint16_t, 2, 4, 4, 1> Small;      // 128 x 64, four
+typedef Cfg<float, 4, 4, 2, 2> F32;           // 128 x 128, four
+
+struct Shape {
+  bool big;
+  int bm, bn, wm;
+};
+Shape shape_of(int64_t rows, bool bf16) {
+  if (!bf16) return {false, F32::BM, F32::BN, F32::WM};
+  if (rows > 128) return {true, Big::BM, Big::BN, Big::WM};
+  return {false, Small::BM, Small::BN, Small::WM};
+}
+
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Vocabulary rows of a piece: P of all rows of x fits PIECE_BYTES, but at least 2048 columns of it; pieces of equal width
+int64_t piece_width(int64_t rows, int64_t vocab, bool bf16) {
+  const int64_t fit = PIECE_BYTES / ((bf16 ? 2 : 4) * rows) / 256 * 256;
+  const int64_t most = fit < 2048 ? 2048 : fit;
+  const int64_t pieces = (vocab + most - 1) / most;
+  return up((vocab + pieces - 1) / pieces, 256);
+}
+
+// dx has few tiles where there are few rows: its contraction is cut until the launch has a workgroup for every compute unit
+int dx_splits(int64_t rows, int64_t width, int64_t cols, const Shape& f) {
+  const int64_t tiles = ((rows + f.bn - 1) / f.bn) * ((cols + f.bm - 1) / f.bm);
+  int64_t s = (256 + tiles - 1) / tiles;
+  const int64_t most = (width + 255) / 256;
+  return (int)(s < 1 ? 1 : s > most ? most : s);
+}
+
+template <class C>
+void logits(const HeadDev& h, hipStream_t s) {
+  const int mt = (int)((h.vocab + C::BM - 1) / C::BM), nt = (int)((h.rows + C::BN - 1) / C::BN);
+  hipLaunchKernelGGL((logits_kernel<C>), dim3((unsigned)(mt * nt)), dim3(C::THREADS), 0, s, h, mt);
+}
+
+template <class C>
+void gradients(const HeadDev& h, int64_t width, int splits, hipStream_t s) {
+  for (int64_t first = 0; first < h.vocab; first += width) {
+    GradPlan g;
+    g.first = first;
+    g.width = (int)(h.vocab - first < width ? h.vocab - first : width);
+    g.pitch = width;
+    const int mp = (int)((up(g.width, 64) + C::BM - 1) / C::BM), np = (int)((h.rows + C::BN - 1) / C::BN);
+    hipLaunchKernelGGL((piece_kernel<C>), dim3((unsigned)(mp * np)), dim3(C::THREADS), 0, s, h, first, g.width, width, mp);
+    g.mt = (h.cols + C::BM - 1) / C::BM;
+    g.splits = h.dx.p ? splits : 0;
+    g.k_split = (int)up((g.width + splits - 1) / splits, 64);
+    g.nt_w = h.dw.p ? (g.width + C::BN - 1) / C::BN : 0;
+    g.begin = first == 0;
+    hipLaunchKernelGGL((grad_kernel<C>), dim3((unsigned)(g.mt * (g.nt_w + np * g.splits))), dim3(C::THREADS), 0, s, h, g);
+  }
+}
+
+void pack(const HeadDev& h, hipStream_t s) {
+  if (h.rows > COUNT_ROWS)
+    hipLaunchKernelGGL(count_kernel, dim3((unsigned)((h.rows + COUNT_ROWS - 1) / COUNT_ROWS)), dim3(256), 0, s, h);
+  const dim3 grid((unsigned)((h.rows + PACK_ROWS - 1) / PACK_ROWS));
+  if (h.bf16) hipLaunchKernelGGL((pack_kernel<uint16_t>), grid, dim3(256), 0, s, h);
+  else hipLaunchKernelGGL((pack_kernel<float>), grid, dim3(256), 0, s, h);
+  if (h.w_packed) {
+    if (h.bf16) hipLaunchKernelGGL((pack_w_kernel<uint16_t>), dim3((unsigned)h.vocab), dim3(256), 0, s, h);
+    else hipLaunchKernelGGL((pack_w_kernel<float>), dim3((unsigned)h.vocab), dim3(256), 0, s, h);
+  }
+}
+
+}  // namespace
+
+HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx) {
+  const int64_t es = bf16 ? 2 : 4, pitch = up(cols, bf16 ? 64 : 32);
+  const Shape f = shape_of(rows, bf16);
+  HeadLayout l;
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t o = at;
+    at += up(bytes, 256);
+    return o;
+  };
+  l.head = take(sizeof(HeadHeader));
+  l.counts = take(4 * ((rows + COUNT_ROWS - 1) / COUNT_ROWS));
+  l.list = take(4 * rows);
+  l.place = take(4 * rows);
+  l.target = take(4 * rows);
+  l.weight = take(4 * rows);
+  l.lse = take(4 * rows);
+  l.x = take(rows * pitch * es);
+  l.w = w_packed ? take(vocab * pitch * es) : -1;
+  l.part = l.hit = l.sums = l.p = l.acc = -1;
+  if (!backward) {
+    l.part = take(8 * rows * ((vocab + f.bm - 1) / f.bm) * f.wm);
+    l.hit = take(4 * rows);
+    l.sums = take(8 * ((rows + 63) / 64));
+  } else {
+    const int64_t width = piece_width(rows > 0 ? rows : 1, vocab, bf16);
+    l.p = take(rows * width * es);
+    if (want_dx) l.acc = take(4 * rows * pitch * dx_splits(rows > 0 ? rows : 1, width, cols, f));
+  }
+  l.bytes = at;
+  return l;
+}
+
+void launch_head_loss(const HeadDev& h, hipStream_t s) {
+  if (h.rows == 0) {
+    hipLaunchKernelGGL(no_rows_loss_kernel, dim3(1), dim3(1), 0, s, h);
+    return;
+  }
+  pack(h, s);
+  const Shape f = shape_of(h.rows, h.bf16);
+  if (!h.bf16) logits<F32>(h, s);
+  else if (f.big) logits<Big>(h, s);
+  else logits<Small>(h, s);
+  const int tiles = (int)((h.vocab + f.bm - 1) / f.bm) * f.wm, groups = (int)((h.rows + 63) / 64);
+  hipLaunchKernelGGL(finish_kernel, dim3((unsigned)groups), dim3(1024), 0, s, h, tiles, groups == 1 ? 1 : 0);
+  if (groups > 1) hipLaunchKernelGGL(total_kernel, dim3(1), dim3(256), 0, s, h, groups);
+}
+
+void launch_head_backward(const HeadDev& h, hipStream_t s) {
+  if (h.rows == 0) {
+    if (!h.dw.p) return;
+    if (h.bf16) hipLaunchKernelGGL((no_rows_dw_kernel<uint16_t>), dim3((unsigned)h.vocab), dim3(256), 0, s, h);
+    else hipLaunchKernelGGL((no_rows_dw_kernel<float>), dim3((unsigned)h.vocab), dim3(256), 0, s, h);
+    return;
+  }
+  pack(h, s);
+  const Shape f = shape_of(h.rows, h.bf16);
+  const int64_t width = piece_width(h.rows, h.vocab, h.bf16);
+  const int splits = dx_splits(h.rows, width, h.cols, f);
+  if (!h.bf16) gradients<F32>(h, width, splits, s);
+  else if (f.big) gradients<Big>(h, width, splits, s);
+  else gradients<Small>(h, width, splits, s);
+  if (h.dx.p) {
+    if (h.bf16) hipLaunchKernelGGL((dx_kernel<uint16_t>), dim3((unsigned)h.rows), dim3(256), 0, s, h, splits);
+    else hipLaunchKernelGGL((dx_kernel<float>), dim3((unsigned)h.rows), dim3(256), 0, s, h, splits);
+  }
+}
+
+}  // namespace adapm

@@ -94,6 +94,10 @@ def main():
     ap.add_argument("--grad-sets", type=int, default=2)
     ap.add_argument("--grad-clip", type=float, default=0.0, help="global gradient-norm clipping threshold (0 = off)")
     ap.add_argument("--rank", type=int, default=0, help="override the rank of every low-rank block (rank / T sweeps)")
+    ap.add_argument("--head-tokens", type=int, default=0,
+                    help="also run the end of the model (residual norm, loss over the vocabulary, gradients of the norm and head "
+                         "blocks) on a batch of that many tokens in front of the steps, and report it (0 = off)")
+    ap.add_argument("--head-dropout", type=float, default=0.1, help="residual dropout of --head-tokens")
     args = ap.parse_args()
     if args.gpus != 1:
         print("bench.py: this build is single-GPU (blocks are independent, the library has no collectives); "
@@ -251,6 +255,29 @@ def main():
                     launches_per_pass=k["launches_per_pass"], traffic=None)
         return roof
 
+    def head_bench():
+        """The end of the model on its own: mean of 10 passes from HIP events; its gradients stay in the gradient sets that the
+        optimizer steps read."""
+        from paper_2510_09103_amd.head import LMHead
+        model_end = LMHead(wl.blocks, p=args.head_dropout)
+        x, residual, targets = WL.head_batch(wl, args.head_tokens, device=dev)
+        for i, grads in enumerate(grad_sets):
+            loss = model_end.step(params, grads, x, residual, targets, i + 1).loss
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        n = 10
+        e0.record()
+        for i in range(n):
+            model_end.step(params, grad_sets[i % len(grad_sets)], x, residual, targets, i + 1)
+        e1.record()
+        torch.cuda.synchronize()
+        ms = e0.elapsed_time(e1) / n
+        b = wl.blocks[model_end.head]
+        products = 8.0 * args.head_tokens * b.numel      # logits, logits again, two gradients
+        return {"tokens": args.head_tokens, "head": [b.rows, b.cols], "dropout": args.head_dropout, "loss": loss.item(), "ms_per_pass": ms,
+                "TFLOPs": products / (ms * 1e-3) / 1e12, "mfma_frac": products / (ms * 1e-3) / 1e12 / MFMA_BF16_PEAK_TFLOPS,
+                "note": "not part of ms_per_step; the gradients of the norm and head blocks that the timed steps read come from it"}
+
+    model_end = head_bench() if args.head_tokens > 0 else None
     opt = make(args.T)
     K, W = args.steps, args.warmup
     for t in range(1, W + 1):
@@ -360,6 +387,8 @@ def main():
         "kernels": kernels,
         "literal_T1": literal,
     }
+    if model_end is not None:
+        out["model_end"] = model_end
     if not args.no_cpu_baseline:
         out["cpu_baseline"] = cpu_baseline(wl, args.T, lr)
     print(json.dumps(out))

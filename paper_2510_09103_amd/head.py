@@ -1,0 +1,59 @@
+"""The end of a model over a block table: residual dropout and addition, final norm, output head and loss, and their gradients written
+into the gradient tensors of the table's blocks, where AdaPM.step reads them.
+
+    h = residual + dropout(x);  y = norm(h) * params[norm];  loss = cross entropy of y params[head]^T
+"""
+from __future__ import annotations
+
+from typing import List, NamedTuple, Optional, Sequence
+
+import torch
+
+from . import ops
+from .workloads import BlockSpec
+
+NORM_NAMES = ("ln_f", "norm_f")              # final norm vector
+HEAD_NAMES = ("lm_head", "wte", "embed")     # output head; the embedding where the table ties them
+
+
+class HeadStep(NamedTuple):
+    loss: torch.Tensor           # fp32, no dimensions
+    row_loss: torch.Tensor       # fp32, one a token
+    dx: torch.Tensor             # gradient of x
+    dresidual: torch.Tensor      # gradient of the residual (dx itself without dropout)
+
+
+class LMHead:
+    """blocks: the table.  p, seed: dropout on x before it is added (GPT-2 runs); every step draws from the counter (seed, t)."""
+
+    def __init__(self, blocks: Sequence[BlockSpec], eps: float = 1e-5, p: float = 0.0, seed: int = 0x5EED):
+        self.norm = self._find(blocks, NORM_NAMES, "final norm")
+        self.head = self._find(blocks, HEAD_NAMES, "output head")
+        n, h = blocks[self.norm], blocks[self.head]
+        if n.numel != h.cols:
+            raise ValueError(f"block {n.name} has {n.numel} elements, {h.name} {h.cols} columns")
+        self.blocks, self.eps, self.p, self.seed = list(blocks), eps, p, seed
+        self.tied = h.name != "lm_head"
+
+    @staticmethod
+    def _find(blocks, names, what):
+        for name in names:
+            for i, b in enumerate(blocks):
+                if b.name == name:
+                    return i
+        raise ValueError(f"the table has no {what} (a block named {', '.join(names)})")
+
+    def step(self, params: List[torch.Tensor], grads: List[torch.Tensor], x: torch.Tensor, residual: Optional[torch.Tensor],
+             targets: torch.Tensor, t: int, row_weight: Optional[torch.Tensor] = None, scale: float = 1.0) -> HeadStep:
+        """Forward and backward pass of step t (1-based) on a batch of hidden states (any leading dimensions, the type of the table's
+        gradients).  Overwrites grads[norm] and grads[head]; where the head is the embedding, what the embedding's look-up adds to
+        that gradient is the caller's to add afterwards.  Parameters of another type (fp32 masters of a bf16 model) are cast first."""
+        rng = ops.Rng(self.seed, t)
+        weight, gain = params[self.head], params[self.norm]
+        if weight.dtype != x.dtype:
+            weight = weight.to(x.dtype)
+        n = ops.rms_norm(x, gain, eps=self.eps, residual=residual, p=self.p, rng=rng)
+        out = ops.head_loss(n.y, weight, targets, row_weight=row_weight, scale=scale)
+        dy, _ = ops.head_backward(n.y, weight, targets, out.lse, row_weight=row_weight, scale=scale, dweight=grads[self.head])
+        dx, dres, _ = ops.rms_norm_backward(dy, n.h, gain, n.rstd, p=self.p, rng=rng, dweight=grads[self.norm])
+        return HeadStep(out.loss, out.row_loss, dx, dres)

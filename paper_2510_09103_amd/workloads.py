@@ -279,3 +279,17 @@ class GradientStream:
             out.append((self.scale * G).to(_TORCH_DT[b.grad_dtype]).contiguous())
         self.t += 1
         return out
+
+
+def head_batch(wl: Workload, tokens: int, masked: float = 0.0, seed: int = 0, device="cpu"):
+    """(x, residual, targets) of a synthetic batch for the end of a model over wl's table (LMHead): what the last layer adds and the
+    residual stream in the table's gradient type, and Zipf-distributed targets of which a share `masked` carries none (-100)."""
+    head = next(b for name in ("lm_head", "wte", "embed") for b in wl.blocks if b.name == name)
+    g = _gen(device, wl.seed, seed, 4)
+    dt = _TORCH_DT[head.grad_dtype]
+    x = torch.randn(tokens, head.cols, device=device, generator=g).to(dt)
+    residual = torch.randn(tokens, head.cols, device=device, generator=g).to(dt)
+    u = torch.rand(tokens, device=device, generator=g, dtype=torch.float64)
+    targets = (head.rows ** u).long().clamp_(1, head.rows) - 1
+    targets[torch.rand(tokens, device=device, generator=g) < masked] = -100
+    return x, residual, targets

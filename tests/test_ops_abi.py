@@ -135,3 +135,28 @@ def test_tensors_are_checked():
             call()
     with pytest.raises(TypeError, match="float32 or bfloat16"):
         ops.dropout(x.half(), 0.1, ops.Rng(1))
+
+
+def test_end_of_a_table_finds_its_blocks():
+    from paper_2510_09103_amd import workloads as WL
+    from paper_2510_09103_amd.head import LMHead
+    for name, norm, last, tied in (("llama_60m", "norm_f", "embed", True), ("gpt2_350m", "ln_f", "wte", True), ("llama_1b", "norm_f", "lm_head", False),
+                                   ("gpt2_1p5b", "ln_f", "lm_head", False), ("llama_350m_paper", "ln_f", "wte", True)):
+        wl = WL.CONFIGS[name]()
+        end = LMHead(wl.blocks)
+        assert (wl.blocks[end.norm].name, wl.blocks[end.head].name, end.tied) == (norm, last, tied)
+    with pytest.raises(ValueError, match="final norm"):
+        LMHead(WL.tiny_block().blocks)
+    with pytest.raises(ValueError, match="columns"):
+        LMHead([b for b in WL.gpt2_350m().blocks if b.name == "ln_f"] + [b for b in WL.llama_1b().blocks if b.name == "lm_head"])
+
+
+def test_head_batch_is_seeded():
+    from paper_2510_09103_amd import workloads as WL
+    wl = WL.llama_60m()
+    x, res, t = WL.head_batch(wl, 300, masked=0.3, seed=4)
+    again = WL.head_batch(wl, 300, masked=0.3, seed=4)
+    assert all(torch.equal(a, b) for a, b in zip((x, res, t), again)) and not torch.equal(x, WL.head_batch(wl, 300, seed=5)[0])
+    assert x.dtype == torch.bfloat16 and x.shape == res.shape == (300, 512)
+    # a binomial share of rows without a target: five standard deviations
+    assert abs((t == -100).float().mean().item() - 0.3) < 5 * (0.21 / 300) ** 0.5 and t.max() < 32000 and t[t != -100].min() >= 0

@@ -351,3 +351,74 @@ def test_captured_into_a_graph():
         assert all(torch.equal(u, v) for u, v in zip(out, eager)), i
         losses.add(out[0].item())
     assert len(losses) == 4
+
+
+@pytest.mark.parametrize("name,vocab", [("llama_60m", None), ("gpt2_350m", 700), ("llama_1b", 1100)])
+def test_end_of_a_table_and_its_optimizer_step(name, vocab):
+    """LMHead writes the gradients of a table's norm and head blocks (tied, untied; fp32 masters, bf16) and AdaPM.step takes them."""
+    from dataclasses import replace
+    from paper_2510_09103_amd import workloads as WL
+    from paper_2510_09103_amd.head import LMHead
+    from paper_2510_09103_amd.optimizer import AdaPM, make_hparams
+    wl = WL.CONFIGS[name]()
+    keep = [b for b in wl.blocks if b.name in ("wte", "embed", "ln_f", "norm_f", "lm_head")]
+    wl = replace(wl, blocks=tuple(replace(b, rows=vocab) if vocab and b.cols > 1 else b for b in keep))
+    params = WL.initial_params(wl, device="cuda")
+    grads = WL.GradientStream(wl, device="cuda").next()
+    before = [g.clone() for g in grads]
+    end = LMHead(wl.blocks, p=0.1)
+    x, res, t = WL.head_batch(wl, 200, masked=0.1, device="cuda")
+    out = end.step(params, grads, x, res, t, 3)
+    W, gain = params[end.head].to(x.dtype), params[end.norm]
+    f = R.factors(200, x.shape[1], 0.1, end.seed, 3).cuda()
+    sum64 = x.double() * f + res.double()
+    n = ops.rms_norm(x, gain, residual=res, p=0.1, rng=ops.Rng(end.seed, 3))
+    # the product and the sum are rounded to fp32 before the rounding to bf16, which can then fall to the other side
+    R.within("h", n.h, sum64, 3 * R.U * ((x.double() * f).abs() + sum64.abs()), x.dtype)
+    h = n.h
+    want = R.head(n.y, W, t, dtype=x.dtype)
+    R.within("loss", out.loss, want["loss"], want["loss_off"])
+    R.within("head", grads[end.head], want["dw"], want["dw_off"], x.dtype)
+    dy = ops.head_backward(n.y, W, t, ops.head_loss(n.y, W, t).lse)[0]
+    dres, size, dg, dg_size = R.norm_backward(dy, h, gain.view(-1), n.rstd)
+    R.within("dresidual", out.dresidual, dres, 80 * R.U * size, x.dtype)
+    R.within("norm", grads[end.norm].view(-1), dg, 91 * R.U * dg_size, grads[end.norm].dtype)
+    for i, (a, b) in enumerate(zip(before, grads)):
+        assert torch.equal(a, b) == (i not in (end.norm, end.head))
+    # the step on these buffers is the step on copies of them
+    copies = [p.clone() for p in params]
+    for p, g in ((params, grads), (copies, [g.clone() for g in grads])):
+        AdaPM(wl.blocks, make_hparams()).step(p, g, 1, 1e-3)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(params, copies))
+
+
+def test_replays_beside_an_eager_optimizer_step():
+    """The end of a model captured into a graph whose gradient buffers an eager AdaPM.step reads between the replays."""
+    from dataclasses import replace
+    from paper_2510_09103_amd import workloads as WL
+    from paper_2510_09103_amd.head import LMHead
+    from paper_2510_09103_amd.optimizer import AdaPM, make_hparams
+    wl = WL.gpt2_350m()
+    wl = replace(wl, blocks=tuple(replace(b, rows=600) if b.name == "wte" else b for b in wl.blocks if b.name in ("wte", "ln_f")))
+    x, res, t = WL.head_batch(wl, 150, device="cuda")
+    runs = []
+    for captured in (False, True):
+        params = WL.initial_params(wl, device="cuda")
+        grads = [torch.zeros_like(p) for p in params]
+        end, opt = LMHead(wl.blocks, p=0.2), AdaPM(wl.blocks, make_hparams())
+        end.step(params, grads, x, res, t, 1)
+        torch.cuda.synchronize()
+        if captured:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                out = end.step(params, grads, x, res, t, 1)
+        for step in range(1, 4):
+            if captured:
+                graph.replay()
+            else:
+                out = end.step(params, grads, x, res, t, 1)
+            opt.step(params, grads, step, 1e-2)
+            torch.cuda.synchronize()
+        runs.append([*params, *grads, out.loss])
+    assert all(torch.equal(a, b) for a, b in zip(*runs))

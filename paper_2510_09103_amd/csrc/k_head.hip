@@ -124,9 +124,9 @@ __global__ __launch_bounds__(256) void pack_w_kernel(HeadDev h) {
 
 // ---- matrix products -------------------------------------------------------------------------------------------------
 // A tile of D[m][n] = sum_k A(m, k) B(n, k).  An operand is stored with k along its rows (KC: element (u, k) at u pitch + k) or
-// across them (at k pitch + u).  128-byte slices of the contraction (64 bf16 or 32 fp32 values) go through two LDS buffers: the
-// next slice is loaded into registers while the current one feeds the matrix cores.  Pieces of 16 bytes are exchanged within an LDS
-// row (by the row's number) so that the reads of a fragment fall on different banks without padding.
+// across them (at k pitch + u).  128-byte slices of the contraction (64 bf16 or 32 fp32 values) are copied straight into one of two
+// LDS buffers, in order; which 16-byte piece of the slice a thread fetches is exchanged (by the LDS row's number) so that the reads
+// of a fragment fall on different banks without padding.
 // bf16: v_mfma_f32_16x16x32, KC fragments are one 16-byte read, the others two transposing reads of 8 bytes.
 // fp32: v_mfma_f32_16x16x4, four of them to a 16-byte read; which k meets which instruction is the same for both operands.
 struct Src {
@@ -143,31 +143,7 @@ struct Operand {
   static constexpr int NL = BYTES / (16 * NTHR);      // 16-byte pieces of a thread
   static constexpr int RPC = BU * ES / 16;            // pieces of a row where k goes across
   static_assert(NL * 16 * NTHR == BYTES, "whole pieces");
-
-  u32x4 r[NL];
-
-  __device__ __forceinline__ void load(const Src& s, int u0, int k0) {
-    const int tid = threadIdx.x;
-    if (KC) {
-      const int rows = s.u - u0 < BU ? s.u - u0 : BU;
-      const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(s.p + (int64_t)u0 * s.pitch), 0, (int)(rows * s.pitch), 0x00020000);
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const int c = tid + NTHR * i, row = c >> 3, ck = c & 7, k = k0 + ck * (16 / ES);
-        r[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, k < s.k ? (int)(row * s.pitch) + k * ES : (int)OOB, 0, 0);
-      }
-    } else {
-      const int rows = s.k - k0 < BK ? s.k - k0 : BK;
-      const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(s.p + (int64_t)k0 * s.pitch), 0, (int)(rows * s.pitch), 0x00020000);
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const int c = tid + NTHR * i, row = c / RPC, u = u0 + (c % RPC) * (16 / ES);
-        r[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, u < s.u ? (int)(row * s.pitch) + u * ES : (int)OOB, 0, 0);
-      }
-    }
-  }
-
-  // Where a piece goes.  KC: its place among the eight of its row is exchanged by the row's number.  Else pieces of 32 bytes (bf16; a
+  // Where a piece stands.  KC: its place among the eight of its row is exchanged by the row's number.  Else pieces of 32 bytes (bf16; a
   // read touches rows 0 .. 3 and 8 .. 11 of a step at a time) or 64 bytes (fp32; rows 0, 4, 8 and 12) are exchanged by the row, over the
   // 256 bytes of all banks: where an LDS row is 128 bytes, its number's lowest bit says which half it lies in already.
   static_assert(KC || (ES == 2 && BU * ES == 128) || BU * ES >= 256, "exchanged inside a row");
@@ -176,21 +152,47 @@ struct Operand {
     return BU * ES == 128 ? ((k >> 1) & 1) | ((k >> 2) & 2) : (k & 3) | ((k >> 1) & 4);
   }
 
-  __device__ __forceinline__ void store(lds_u8* lds) const {
+  int off[NL];          // byte offset of a thread's pieces in the slice that starts at k = 0, OOB outside the free index
+  int k_in;             // KC: place of its pieces in the slice (the same for all)
+  const char* base;
+
+  __device__ __forceinline__ void init(const Src& s, int u0) {
     const int tid = threadIdx.x;
+    k_in = 0;
+    if (KC) {
+      base = s.p + (int64_t)u0 * s.pitch;
+      k_in = ((tid & 7) ^ ((tid >> 3) & 7)) * (16 / ES);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) off[i] = ((tid + NTHR * i) >> 3) * (int)s.pitch + k_in * ES;
+    } else {
+      base = s.p;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int c = tid + NTHR * i, row = c / RPC, at = c % RPC;
+        const int cu = ES == 2 ? ((at >> 1) ^ swz(row)) << 1 | (at & 1) : ((at >> 2) ^ swz(row)) << 2 | (at & 3);
+        const int u = u0 + cu * (16 / ES);
+        off[i] = u < s.u ? row * (int)s.pitch + u * ES : (int)OOB;
+      }
+    }
+  }
+
+  // asynchronous copy of the slice at k0; a lane outside the operand gets zeros
+  __device__ __forceinline__ void copy(const Src& s, int u0, int k0, lds_u8* lds) const {
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    int rows;
+    const char* from;
+    if (KC) {
+      rows = s.u - u0 < BU ? s.u - u0 : BU;
+      from = base;
+    } else {
+      rows = s.k - k0 < BK ? s.k - k0 : BK;
+      from = base + (int64_t)k0 * s.pitch;
+    }
+    const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, (int)(rows * s.pitch), 0x00020000);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int c = tid + NTHR * i;
-      int at;
-      if (KC) {
-        const int row = c >> 3, ck = c & 7;
-        at = row * 128 + ((ck ^ (row & 7)) << 4);
-      } else {
-        const int row = c / RPC, cu = c % RPC;
-        at = ES == 2 ? row * (BU * ES) + ((((cu >> 1) ^ swz(row)) << 1 | (cu & 1)) << 4)
-                     : row * (BU * ES) + ((((cu >> 2) ^ swz(row)) << 2 | (cu & 3)) << 4);
-      }
-      *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(lds + at) = r[i];
+      const int o = KC ? (k0 + k_in < s.k ? off[i] + k0 * ES : (int)OOB) : off[i];
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(lds + (NTHR * i + 64 * wave) * 16), 16, o, 0, 0, 0);
     }
   }
 };
@@ -252,13 +254,48 @@ struct Acc {
   f32x4 v[C::MT][C::NT];
 };
 
-// acc = the tile at (m0, n0), contraction over [k0, k1)
+template <class C, bool AKC, bool BKC>
+struct Frags {
+  u32x4 a[C::MT], b[C::NT];
+  __device__ __forceinline__ void read(const lds_u8* la, const lds_u8* lb, int um, int un, int ks) {
+#pragma unroll
+    for (int j = 0; j < C::NT; ++j) b[j] = fragment<typename C::T, C::BN, BKC>(lb, un + 16 * j, ks);
+#pragma unroll
+    for (int i = 0; i < C::MT; ++i) a[i] = fragment<typename C::T, C::BM, AKC>(la, um + 16 * i, ks);
+  }
+  // rows [first, last) of the wave's tiles
+  __device__ __forceinline__ void multiply(Acc<C>& acc, int first, int last) const {
+#pragma unroll
+    for (int i = 0; i < C::MT; ++i)
+      if (i >= first && i < last) {
+#pragma unroll
+        for (int j = 0; j < C::NT; ++j) acc.v[i][j] = mma(a[i], b[j], acc.v[i][j], (const typename C::T*)nullptr);
+      }
+  }
+};
+
+// Order of a stretch of code, as the compiler is told it: N times one LDS read (0x100) or one copy (0x010) and M matrix instructions.
+template <int KIND, int N, int M>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(KIND, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
+  }
+}
+
+// acc = the tile at (m0, n0), contraction over [k0, k1).  A slice is two steps of fragments.  While the first step's are multiplied the
+// second's are read and the next slice is on its way into the other buffer; it has to be there, and every wavefront done with this one,
+// a quarter into the second step, whose rest covers the reads of the next slice's first.  The reads stand before the copies so that
+// none of them waits for one.
 template <class C, bool AKC, bool BKC>
 __device__ __forceinline__ void product(const Src& A, const Src& B, int m0, int n0, int k0, int k1, lds_u8* lds, Acc<C>& acc) {
   typedef typename C::T T;
   typedef Operand<T, C::BM, C::THREADS, AKC> OA;
   typedef Operand<T, C::BN, C::THREADS, BKC> OB;
-  constexpr int HALF = OA::BYTES + OB::BYTES;
+  constexpr int HALF = OA::BYTES + OB::BYTES, EARLY = C::MT / 4 > 0 ? C::MT / 4 : 1;
+  constexpr int ACROSS = sizeof(T) == 2 ? 2 : 4, READS = C::MT * (AKC ? 1 : ACROSS) + C::NT * (BKC ? 1 : ACROSS);
+  constexpr int MUL = C::NT * (sizeof(T) == 2 ? 1 : 4);          // matrix instructions of a row of tiles
   const int wave = threadIdx.x >> 6, um = (wave % C::WM) * 16 * C::MT, un = (wave / C::WM) * 16 * C::NT;
 #pragma unroll
   for (int i = 0; i < C::MT; ++i)
@@ -267,40 +304,35 @@ __device__ __forceinline__ void product(const Src& A, const Src& B, int m0, int 
   if (k0 >= k1) return;
   OA a;
   OB b;
-  a.load(A, m0, k0);
-  b.load(B, n0, k0);
-  __syncthreads();                       // the buffers' last readers
-  a.store(lds);
-  b.store(lds + OA::BYTES);
+  a.init(A, m0);
+  b.init(B, n0);
+  a.copy(A, m0, k0, lds);
+  b.copy(B, n0, k0, lds + OA::BYTES);
   __syncthreads();
-  int buf = 0;
-  for (int k = k0; k < k1; k += OA::BK) {
-    const bool more = k + OA::BK < k1;
-    if (more) {
-      a.load(A, m0, k + OA::BK);
-      b.load(B, n0, k + OA::BK);
-    }
-    const lds_u8* la = lds + buf * HALF;
-    const lds_u8* lb = la + OA::BYTES;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      u32x4 fa[C::MT], fb[C::NT];
-#pragma unroll
-      for (int j = 0; j < C::NT; ++j) fb[j] = fragment<T, C::BN, BKC>(lb, un + 16 * j, ks);
-#pragma unroll
-      for (int i = 0; i < C::MT; ++i) fa[i] = fragment<T, C::BM, AKC>(la, um + 16 * i, ks);
-#pragma unroll
-      for (int i = 0; i < C::MT; ++i)
-#pragma unroll
-        for (int j = 0; j < C::NT; ++j) acc.v[i][j] = mma(fa[i], fb[j], acc.v[i][j], (const T*)nullptr);
-    }
-    buf ^= 1;
-    if (more) {
-      a.store(lds + buf * HALF);
-      b.store(lds + buf * HALF + OA::BYTES);
-    }
+  Frags<C, AKC, BKC> f0, f1;
+  f0.read(lds, lds + OA::BYTES, um, un, 0);
+  int buf = 0, k = k0;
+  for (; k + OA::BK < k1; k += OA::BK) {
+    const lds_u8* now = lds + buf * HALF;
+    lds_u8* next = lds + (buf ^ 1) * HALF;
+    f1.read(now, now + OA::BYTES, um, un, 1);
+    a.copy(A, m0, k + OA::BK, next);
+    b.copy(B, n0, k + OA::BK, next + OA::BYTES);
+    f0.multiply(acc, 0, C::MT);
+    f1.multiply(acc, 0, EARLY);
+    interleave<0x100, READS, 1>();
+    interleave<0x010, OA::NL + OB::NL, 1>();
+    __builtin_amdgcn_sched_barrier(0);
     __syncthreads();
+    f0.read(next, next + OA::BYTES, um, un, 0);
+    f1.multiply(acc, EARLY, C::MT);
+    interleave<0x100, READS, ((C::MT - EARLY) * MUL + READS - 1) / READS>();
+    __builtin_amdgcn_sched_barrier(0);
+    buf ^= 1;
   }
+  f1.read(lds + buf * HALF, lds + buf * HALF + OA::BYTES, um, un, 1);
+  f0.multiply(acc, 0, C::MT);
+  f1.multiply(acc, 0, C::MT);
 }
 
 // Order of the tiles of a launch: workgroup i runs on XCD i mod 8, which gets a run of neighbouring tiles, eight along n for each

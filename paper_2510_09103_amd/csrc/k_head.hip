@@ -66,6 +66,22 @@ __global__ __launch_bounds__(256) void count_kernel(HeadDev h) {
   if (threadIdx.x == 0) reinterpret_cast<int*>(h.ws + h.lay.counts)[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
 }
 
+typedef u32x4 u32x4_e2 __attribute__((aligned(2), may_alias));
+
+// elements c0 .. of a row of `cols` as 16 bytes, zeros behind its end
+template <class T>
+__device__ __forceinline__ u32x4 piece_of(const T* row, int c0, int cols) {
+  constexpr int V = 16 / sizeof(T);
+  if (c0 + V <= cols) return *reinterpret_cast<const u32x4_e2*>(row + c0);
+  union {
+    T t[V];
+    u32x4 v;
+  } r;
+#pragma unroll
+  for (int i = 0; i < V; ++i) r.t[i] = c0 + i < cols ? row[c0 + i] : T(0);
+  return r.v;
+}
+
 // Places of the rows that count (in their order) and their packed copies.  A workgroup finds how many stand before its own from
 // the counts of the thousands before and from the targets of its own thousand.
 template <class T>
@@ -105,21 +121,29 @@ __global__ __launch_bounds__(256) void pack_kernel(HeadDev h) {
     if (threadIdx.x == 0 && r0 + PACK_ROWS >= h.rows) reinterpret_cast<HeadHeader*>(h.ws + h.lay.head)->n = before + __popcll(m);
   }
   __syncthreads();
-  T* out = reinterpret_cast<T*>(h.ws + h.lay.x);
-  const T* x = reinterpret_cast<const T*>(h.x.p);
-  for (int i = 0; i < PACK_ROWS; ++i) {
-    if (r0 + i >= h.rows || place[i] < 0) continue;
-    for (int c2 = threadIdx.x; c2 < h.pitch; c2 += 256)
-      out[(int64_t)place[i] * h.pitch + c2] = c2 < h.cols ? x[(r0 + i) * h.x.stride + c2] : T(0);
+  // pieces of 16 bytes of all the rows at once, whatever alignment x has; zeros behind its columns
+  constexpr int V = 16 / sizeof(T);
+  const int per = h.pitch / V;
+  for (int i = threadIdx.x; i < PACK_ROWS * per; i += 256) {
+    const int r = i / per, c0 = (i - r * per) * V;
+    if (r0 + r >= h.rows || place[r] < 0) continue;
+    *reinterpret_cast<u32x4*>(reinterpret_cast<T*>(h.ws + h.lay.x) + (int64_t)place[r] * h.pitch + c0) =
+        piece_of(reinterpret_cast<const T*>(h.x.p) + (r0 + r) * h.x.stride, c0, h.cols);
   }
 }
 
 // W with rows that are no whole, aligned vectors
 template <class T>
 __global__ __launch_bounds__(256) void pack_w_kernel(HeadDev h) {
-  T* out = reinterpret_cast<T*>(h.ws + h.lay.w) + (int64_t)blockIdx.x * h.pitch;
-  const T* w = reinterpret_cast<const T*>(h.w.p) + (int64_t)blockIdx.x * h.w.stride;
-  for (int c = threadIdx.x; c < h.pitch; c += 256) out[c] = c < h.cols ? w[c] : T(0);
+  constexpr int V = 16 / sizeof(T);
+  const int per = h.pitch / V;
+  const int64_t r0 = (int64_t)blockIdx.x * PACK_ROWS;
+  for (int i = threadIdx.x; i < PACK_ROWS * per; i += 256) {
+    const int r = i / per, c0 = (i - r * per) * V;
+    if (r0 + r >= h.vocab) return;
+    *reinterpret_cast<u32x4*>(reinterpret_cast<T*>(h.ws + h.lay.w) + (r0 + r) * h.pitch + c0) =
+        piece_of(reinterpret_cast<const T*>(h.w.p) + (r0 + r) * h.w.stride, c0, h.cols);
+  }
 }
 
 // ---- matrix products -------------------------------------------------------------------------------------------------
@@ -415,16 +439,20 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_
   }
 }
 
-// joins the tiles' maxima and sums of 64 rows: 16 wavefronts share the tiles; each row's loss, and the workgroup's sum of them
+// Joins the tiles' maxima and sums: RL rows a workgroup, whose 1024 / RL slices share the tiles; each row's loss, and the workgroup's
+// sum of them.  Up to 8 rows take 128 slices (one row over 32000 columns: 28.5 us with 16 of them, a chain of 63 loads), more rows
+// 16, whose loads are whole lines.
+template <int RL>
 __global__ __launch_bounds__(1024) void finish_kernel(HeadDev h, int tiles, int last) {
-  __shared__ float rm[16][64], rs[16][64];
+  constexpr int SL = 1024 / RL;
+  __shared__ float rm[SL][RL], rs[SL][RL];
   const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, row = blockIdx.x * 64 + l;
+  const int l = threadIdx.x % RL, w = threadIdx.x / RL, row = blockIdx.x * RL + l;
   const float2* part = reinterpret_cast<const float2*>(h.ws + h.lay.part);
   double* sums = reinterpret_cast<double*>(h.ws + h.lay.sums);
   float m = -INFINITY, s = 0.f;
   if (row < n)
-    for (int t = w; t < tiles; t += 16) {
+    for (int t = w; t < tiles; t += SL) {
       const float2 p = part[(int64_t)t * h.rows + row];
       if (p.y == 0.f) continue;                        // a tile behind the vocabulary's end
       const float top = fmaxf(m, p.x);
@@ -434,18 +462,21 @@ __global__ __launch_bounds__(1024) void finish_kernel(HeadDev h, int tiles, int 
   rm[w][l] = m;
   rs[w][l] = s;
   __syncthreads();
-  if (w) return;
+#pragma unroll
+  for (int o = SL / 2; o > 0; o >>= 1) {
+    if (w < o) {
+      const float m2 = rm[w + o][l], s2 = rs[w + o][l], top = fmaxf(m, m2);
+      s = (s == 0.f ? 0.f : s * __builtin_amdgcn_exp2f((m - top) * LOG2E)) + (s2 == 0.f ? 0.f : s2 * __builtin_amdgcn_exp2f((m2 - top) * LOG2E));
+      rm[w][l] = m = top;
+      rs[w][l] = s;
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x >= 64) return;
   double part_loss = 0.0;
-  if (row < n) {
-    float top = rm[0][l];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, rm[i][l]);
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (rs[i][l] != 0.f) sum += rs[i][l] * __builtin_amdgcn_exp2f((rm[i][l] - top) * LOG2E);
+  if (w == 0 && row < n) {
     // the difference of the logits first, which is exact where they are near: a small loss keeps its digits
-    const float log_sum = logf(sum), lse = top + log_sum, loss = (top - reinterpret_cast<const float*>(h.ws + h.lay.hit)[row]) + log_sum;
+    const float log_sum = logf(s), lse = m + log_sum, loss = (m - reinterpret_cast<const float*>(h.ws + h.lay.hit)[row]) + log_sum;
     const int to = reinterpret_cast<const int*>(h.ws + h.lay.list)[row];
     h.lse[to] = lse;
     h.row_loss[to] = loss;
@@ -453,7 +484,7 @@ __global__ __launch_bounds__(1024) void finish_kernel(HeadDev h, int tiles, int 
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) part_loss += __shfl_xor(part_loss, o);
-  if (l) return;
+  if (threadIdx.x) return;
   if (last) *h.loss = (float)(part_loss * (double)h.scale / (h.mean ? (double)(n > 0 ? n : 1) : 1.0));
   else sums[blockIdx.x] = part_loss;
 }
@@ -695,8 +726,9 @@ void pack(const HeadDev& h, hipStream_t s) {
   if (h.bf16) hipLaunchKernelGGL((pack_kernel<uint16_t>), grid, dim3(256), 0, s, h);
   else hipLaunchKernelGGL((pack_kernel<float>), grid, dim3(256), 0, s, h);
   if (h.w_packed) {
-    if (h.bf16) hipLaunchKernelGGL((pack_w_kernel<uint16_t>), dim3((unsigned)h.vocab), dim3(256), 0, s, h);
-    else hipLaunchKernelGGL((pack_w_kernel<float>), dim3((unsigned)h.vocab), dim3(256), 0, s, h);
+    const dim3 wgrid((unsigned)((h.vocab + PACK_ROWS - 1) / PACK_ROWS));
+    if (h.bf16) hipLaunchKernelGGL((pack_w_kernel<uint16_t>), wgrid, dim3(256), 0, s, h);
+    else hipLaunchKernelGGL((pack_w_kernel<float>), wgrid, dim3(256), 0, s, h);
   }
 }
 
@@ -746,7 +778,8 @@ void launch_head_loss(const HeadDev& h, hipStream_t s) {
   else if (f.big) logits<Big>(h, s);
   else logits<Small>(h, s);
   const int tiles = (int)((h.vocab + f.bm - 1) / f.bm) * f.wm, groups = (int)((h.rows + 63) / 64);
-  hipLaunchKernelGGL(finish_kernel, dim3((unsigned)groups), dim3(1024), 0, s, h, tiles, groups == 1 ? 1 : 0);
+  if (h.rows <= 8) hipLaunchKernelGGL((finish_kernel<8>), dim3(1), dim3(1024), 0, s, h, tiles, 1);
+  else hipLaunchKernelGGL((finish_kernel<64>), dim3((unsigned)groups), dim3(1024), 0, s, h, tiles, groups == 1 ? 1 : 0);
   if (groups > 1) hipLaunchKernelGGL(total_kernel, dim3(1), dim3(256), 0, s, h, groups);
 }
 

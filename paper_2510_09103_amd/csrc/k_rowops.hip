@@ -362,19 +362,25 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(NormDev a) {
   }
 }
 
-// dweight[c] = sum over the workgroups' partial sums: 64 columns x 16 slices of the workgroups, slices added in order
+// dweight[c] = sum over the workgroups' partial sums: 16 columns x 64 slices of the workgroups, joined in a fixed order.  (64 columns x 16
+// slices: 20.8 us for 1024 x 2048 partial sums on 32 workgroups.)
 __global__ __launch_bounds__(1024) void norm_dweight_kernel(const float* __restrict__ partial, int groups, int cols, void* out, int bf16) {
-  __shared__ float red[16][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), sl = threadIdx.x >> 6;
+  __shared__ float red[64][17];
+  const int l = threadIdx.x & 15, sl = threadIdx.x >> 4, c = blockIdx.x * 16 + l;
   float s = 0.f;
-  if (c < cols)
-    for (int g = sl; g < groups; g += 16) s += partial[(int64_t)g * cols + c];
-  red[sl][threadIdx.x & 63] = s;
+  if (c < cols) {
+#pragma unroll 4
+    for (int g = sl; g < groups; g += 64) s += partial[(int64_t)g * cols + c];
+  }
+  red[sl][l] = s;
   __syncthreads();
-  if (sl == 0 && c < cols) {
-    float v = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v += red[i][threadIdx.x];
+  for (int o = 32; o > 0; o >>= 1) {
+    if (sl < o) red[sl][l] += red[sl + o][l];
+    __syncthreads();
+  }
+  if (sl == 0 && c < cols) {
+    const float v = red[0][l];
     if (bf16) store1(reinterpret_cast<uint16_t*>(out) + c, v);
     else reinterpret_cast<float*>(out)[c] = v;
   }
@@ -424,7 +430,7 @@ void norm_backward(const NormDev& n, hipStream_t s) {
     else if (f.nv == 4) hipLaunchKernelGGL((norm_backward_kernel<T, 256, 4>), grid, block, 0, s, n);
     else hipLaunchKernelGGL((norm_backward_kernel<T, 256, 8>), grid, block, 0, s, n);
   }
-  hipLaunchKernelGGL(norm_dweight_kernel, dim3((unsigned)((n.cols + 63) / 64)), dim3(1024), 0, s, n.partial, groups, n.cols, n.dweight, n.g_bf16);
+  hipLaunchKernelGGL(norm_dweight_kernel, dim3((unsigned)((n.cols + 15) / 16)), dim3(1024), 0, s, n.partial, groups, n.cols, n.dweight, n.g_bf16);
 }
 
 template <class T>

@@ -148,11 +148,17 @@ __global__ __launch_bounds__(256) void pack_w_kernel(HeadDev h) {
 
 // ---- matrix products -------------------------------------------------------------------------------------------------
 // A tile of D[m][n] = sum_k A(m, k) B(n, k).  An operand is stored with k along its rows (KC: element (u, k) at u pitch + k) or
-// across them (at k pitch + u).  128-byte slices of the contraction (64 bf16 or 32 fp32 values) are copied straight into one of two
-// LDS buffers, in order; which 16-byte piece of the slice a thread fetches is exchanged (by the LDS row's number) so that the reads
-// of a fragment fall on different banks without padding.
+// across them (at k pitch + u).  128-byte slices of the contraction (64 bf16 or 32 fp32 values, two steps of fragments: whole cache lines
+// where k goes along the rows) are copied straight into one of two LDS buffers; which 16-byte piece of a slice a thread fetches is
+// exchanged (by the LDS row's number) so that the reads of a fragment fall on different banks without padding.
 // bf16: v_mfma_f32_16x16x32, KC fragments are one 16-byte read, the others two transposing reads of 8 bytes.
 // fp32: v_mfma_f32_16x16x4, four of them to a 16-byte read; which k meets which instruction is the same for both operands.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t a = (uint64_t)p;
+  return (const char*)((uint64_t)(uint32_t)uniform((int)(uint32_t)(a >> 32)) << 32 | (uint32_t)uniform((int)(uint32_t)a));
+}
+
 struct Src {
   const char* p;        // element (0, 0)
   int64_t pitch;        // bytes
@@ -200,56 +206,53 @@ struct Operand {
     }
   }
 
-  // asynchronous copy of the slice at k0; a lane outside the operand gets zeros
-  __device__ __forceinline__ void copy(const Src& s, int u0, int k0, lds_u8* lds) const {
+  // Asynchronous copy of the slice at k0.  A lane outside the operand gets zeros, and so do all of them at and behind `end` (<= s.k): every
+  // slice is the same number of copies, which is what the waits count.
+  __device__ __forceinline__ void copy(const Src& s, int u0, int k0, int end, lds_u8* lds) const {
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    int rows;
-    const char* from;
-    if (KC) {
-      rows = s.u - u0 < BU ? s.u - u0 : BU;
-      from = base;
-    } else {
-      rows = s.k - k0 < BK ? s.k - k0 : BK;
-      from = base + (int64_t)k0 * s.pitch;
-    }
-    const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, (int)(rows * s.pitch), 0x00020000);
+    const int left = end - k0, rows = KC ? (s.u - u0 < BU ? s.u - u0 : BU) : left < 0 ? 0 : left < BK ? left : BK;
+    const char* from = KC ? base : base + (int64_t)k0 * s.pitch;      // formed, not read, behind the end
+    // uniform values that the compiler may have worked out in vector registers
+    const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(uniform(from)), 0, uniform(rows * (int)s.pitch), 0x00020000);
+    const bool in = k_in < left;
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int o = KC ? (k0 + k_in < s.k ? off[i] + k0 * ES : (int)OOB) : off[i];
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(lds + (NTHR * i + 64 * wave) * 16), 16, o, 0, 0, 0);
-    }
+    for (int i = 0; i < NL; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(lds + (NTHR * i + 64 * wave) * 16), 16,
+                                               !KC || in ? off[i] : (int)OOB, KC ? uniform(k0 * ES) : 0, 0, 0);
   }
 };
 
-// fragment of 16 rows u .. u + 15: eight (bf16) or four (fp32) values of the contraction of step ks for this lane
+// Fragment of 16 rows u .. u + 15 for step ks of a slice: eight (bf16) or four (fp32) values of the contraction for this lane.  `place` is
+// the lane's byte for ks = 0 and u = u0, the first row of the wavefront, the fragment's rows are u0 + 16 i: u0 / 16 is a multiple of the number of fragments, a
+// power of two, so that i can be exchanged with the lane's number by the same exclusive or.
 template <class T, int BU, bool KC>
-__device__ __forceinline__ u32x4 fragment(const lds_u8* lds, int u, int ks) {
+__device__ __forceinline__ int fragment_place(int u0) {
   constexpr int ES = sizeof(T);
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
-  if (KC) {
-    const int row = u + l16, ck = ks * 4 + q;
-    return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(lds + row * 128 + ((ck ^ (row & 7)) << 4));
-  }
+  if (KC) return (u0 + l16) * 128 + ((q ^ (l16 & 7)) << 4);
+  // bf16: lane s of a block of 16 points at row s / 4, columns 4 (s % 4) .. + 3 of a 4 x 16 tile; lane i receives column i of the four rows
+  const int k = ES == 2 ? q * 8 + (l16 >> 2) : q * 4;
+  const int block = (u0 >> 4) ^ Operand<T, BU, 64, KC>::swz(k);
+  return k * (BU * ES) + (ES == 2 ? (block << 5) + ((l16 & 3) << 3) : (block << 6) + (l16 << 2));
+}
+template <class T, int BU, bool KC>
+__device__ __forceinline__ u32x4 fragment(const lds_u8* lds, int place, int i, int ks) {
+  constexpr int ES = sizeof(T);
+  if (KC) return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(lds + (place ^ (ks << 6)) + i * 2048);
+  lds += ks * (64 / ES) * (BU * ES);
   union {
     s16x4 h[2];
     float f[4];
     u32x4 v;
   } r;
   if (ES == 2) {
-    // lane s of a block of 16 points at row s / 4, columns 4 (s % 4) .. + 3 of a 4 x 16 tile; lane i receives column i of the four rows
+    const lds_u8* p = lds + (place ^ (i << 5));
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int k = ks * 32 + q * 8 + h * 4 + (l16 >> 2), c = u + (l16 & 3) * 4;
-      const int at = k * (BU * ES) + (((c >> 4) ^ Operand<T, BU, 64, KC>::swz(k)) << 5) + ((c & 15) << 1);
-      r.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(lds + at));
-    }
+    for (int h = 0; h < 2; ++h) r.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + h * 4 * (BU * ES)));
   } else {
+    const lds_u8* p = lds + (place ^ (i << 6));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int k = ks * 16 + q * 4 + j, c = u + l16;
-      const int at = k * (BU * ES) + (((c >> 4) ^ Operand<T, BU, 64, KC>::swz(k)) << 6) + ((c & 15) << 2);
-      r.f[j] = *reinterpret_cast<const __attribute__((address_space(3))) float*>(lds + at);
-    }
+    for (int j = 0; j < 4; ++j) r.f[j] = *reinterpret_cast<const __attribute__((address_space(3))) float*>(p + j * (BU * ES));
   }
   return r.v;
 }
@@ -270,7 +273,14 @@ struct Cfg {
   typedef T_ T;
   static constexpr int MT = MT_, NT = NT_, WM = WM_, WN = WN_;
   static constexpr int BM = 16 * MT * WM, BN = 16 * NT * WN, THREADS = 64 * WM * WN;
-  static constexpr int LDS = 2 * (BM + BN) * 128;
+  static constexpr int SLICE = (BM + BN) * 128;
+};
+// the two buffers, as arrays of their own: the compiler then knows which copies a read has to wait for
+#define HEAD_BUFFERS                                                                                          \
+  __shared__ __attribute__((aligned(128))) unsigned char buffer0[C::SLICE], buffer1[C::SLICE];                \
+  const Buffers lds{(lds_u8*)buffer0, (lds_u8*)buffer1};
+struct Buffers {
+  lds_u8 *p0, *p1;
 };
 
 template <class C>
@@ -278,85 +288,113 @@ struct Acc {
   f32x4 v[C::MT][C::NT];
 };
 
+// What the wavefronts of a tile do.  A slice is four phases, each half of the wavefront's rows of tiles in one step: read the fragments,
+// multiply them.  With eight wavefronts there are two on each SIMD, and those of the second half of the workgroup are kept
+// one half of a phase behind the first: while one multiplies, with priority, the other reads, and the matrix cores are not left waiting
+// for either.  The barriers between the halves of the phases hold them so.  With four wavefronts the workgroups on a compute unit do
+// that for one another by chance.
+// In the first two phases the next slice is copied into the other buffer; before the last multiplication every wavefront has seen its
+// own copies arrive and its last fragments leave the buffer that the next copies go to.
 template <class C, bool AKC, bool BKC>
-struct Frags {
-  u32x4 a[C::MT], b[C::NT];
-  __device__ __forceinline__ void read(const lds_u8* la, const lds_u8* lb, int um, int un, int ks) {
-#pragma unroll
-    for (int j = 0; j < C::NT; ++j) b[j] = fragment<typename C::T, C::BN, BKC>(lb, un + 16 * j, ks);
-#pragma unroll
-    for (int i = 0; i < C::MT; ++i) a[i] = fragment<typename C::T, C::BM, AKC>(la, um + 16 * i, ks);
-  }
-  // rows [first, last) of the wave's tiles
-  __device__ __forceinline__ void multiply(Acc<C>& acc, int first, int last) const {
-#pragma unroll
-    for (int i = 0; i < C::MT; ++i)
-      if (i >= first && i < last) {
-#pragma unroll
-        for (int j = 0; j < C::NT; ++j) acc.v[i][j] = mma(a[i], b[j], acc.v[i][j], (const typename C::T*)nullptr);
-      }
-  }
-};
-
-// Order of a stretch of code, as the compiler is told it: N times one LDS read (0x100) or one copy (0x010) and M matrix instructions.
-template <int KIND, int N, int M>
-__device__ __forceinline__ void interleave() {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    __builtin_amdgcn_sched_group_barrier(KIND, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
-  }
-}
-
-// acc = the tile at (m0, n0), contraction over [k0, k1).  A slice is two steps of fragments.  While the first step's are multiplied the
-// second's are read and the next slice is on its way into the other buffer; it has to be there, and every wavefront done with this one,
-// a quarter into the second step, whose rest covers the reads of the next slice's first.  The reads stand before the copies so that
-// none of them waits for one.
-template <class C, bool AKC, bool BKC>
-__device__ __forceinline__ void product(const Src& A, const Src& B, int m0, int n0, int k0, int k1, lds_u8* lds, Acc<C>& acc) {
+struct Product {
   typedef typename C::T T;
   typedef Operand<T, C::BM, C::THREADS, AKC> OA;
   typedef Operand<T, C::BN, C::THREADS, BKC> OB;
-  constexpr int HALF = OA::BYTES + OB::BYTES, EARLY = C::MT / 4 > 0 ? C::MT / 4 : 1;
-  constexpr int ACROSS = sizeof(T) == 2 ? 2 : 4, READS = C::MT * (AKC ? 1 : ACROSS) + C::NT * (BKC ? 1 : ACROSS);
-  constexpr int MUL = C::NT * (sizeof(T) == 2 ? 1 : 4);          // matrix instructions of a row of tiles
-  const int wave = threadIdx.x >> 6, um = (wave % C::WM) * 16 * C::MT, un = (wave / C::WM) * 16 * C::NT;
+  static constexpr int BK = OA::BK, HALF = C::MT / 2;
+  static constexpr bool PAIRED = C::THREADS == 512;
+  static_assert(C::MT % 2 == 0, "two halves");
+  const Src A, B;
+  const int m0, n0, k1;
+  const int pa, pb;       // places of the lane's fragments in a slice
+  OA a;
+  OB b;
+
+  static __device__ __forceinline__ void barrier() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  static __device__ __forceinline__ void turn() {
+    if (PAIRED) barrier();
+  }
+  __device__ __forceinline__ void read_a(u32x4 (&f)[HALF], const lds_u8* slice, int half, int ks) const {
+    int place = pa;
+    asm volatile("" : "+v"(place));      // worked out here every time: kept for all fragments the addresses would take too many registers
+#pragma unroll
+    for (int i = 0; i < HALF; ++i) f[i] = fragment<T, C::BM, AKC>(slice, place, half * HALF + i, ks);
+  }
+  __device__ __forceinline__ void read_b(u32x4 (&f)[C::NT], const lds_u8* slice, int ks) const {
+    int place = pb;
+    asm volatile("" : "+v"(place));
+#pragma unroll
+    for (int j = 0; j < C::NT; ++j) f[j] = fragment<T, C::BN, BKC>(slice + OA::BYTES, place, j, ks);
+  }
+  static __device__ __forceinline__ void multiply(const u32x4 (&fa)[HALF], const u32x4 (&fb)[C::NT], Acc<C>& acc, int half) {
+    if (PAIRED) __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int i = 0; i < HALF; ++i)
+#pragma unroll
+      for (int j = 0; j < C::NT; ++j) acc.v[half * HALF + i][j] = mma(fa[i], fb[j], acc.v[half * HALF + i][j], (const T*)nullptr);
+    if (PAIRED) __builtin_amdgcn_s_setprio(0);
+  }
+  // the slice at k in `now`; the next one goes to `next`
+  __device__ __forceinline__ void slice(int k, const lds_u8* __restrict now, lds_u8* __restrict next, Acc<C>& acc) const {
+    u32x4 fa[HALF], fb[C::NT];
+    read_b(fb, now, 0);
+    read_a(fa, now, 0, 0);
+    a.copy(A, m0, k + BK, k1, next);
+    turn();
+    multiply(fa, fb, acc, 0);
+    turn();
+    read_a(fa, now, 1, 0);
+    b.copy(B, n0, k + BK, k1, next + OA::BYTES);
+    turn();
+    multiply(fa, fb, acc, 1);
+    turn();
+    read_b(fb, now, 1);
+    read_a(fa, now, 0, 1);
+    turn();
+    multiply(fa, fb, acc, 0);
+    turn();
+    read_a(fa, now, 1, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    barrier();
+    multiply(fa, fb, acc, 1);
+    turn();
+  }
+  __device__ __forceinline__ void run(int k0, const Buffers& lds, Acc<C>& acc) {
+    a.init(A, m0);
+    b.init(B, n0);
+    a.copy(A, m0, k0, k1, lds.p0);
+    b.copy(B, n0, k0, k1, lds.p0 + OA::BYTES);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    barrier();
+    const bool second = PAIRED && uniform((int)threadIdx.x) >= 256;
+    if (second) barrier();
+    for (int k = k0;;) {
+      slice(k, lds.p0, lds.p1, acc);
+      if ((k += BK) >= k1) break;
+      slice(k, lds.p1, lds.p0, acc);
+      if ((k += BK) >= k1) break;
+    }
+    if (PAIRED && !second) barrier();
+  }
+};
+
+// acc = the tile at (m0, n0), contraction over [k0, k1)
+template <class C, bool AKC, bool BKC>
+__device__ __forceinline__ void product(const Src& A, const Src& B, int m0, int n0, int k0, int k1, const Buffers& lds, Acc<C>& acc) {
+  const int wave = threadIdx.x >> 6;
 #pragma unroll
   for (int i = 0; i < C::MT; ++i)
 #pragma unroll
     for (int j = 0; j < C::NT; ++j) acc.v[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (k0 >= k1) return;
-  OA a;
-  OB b;
-  a.init(A, m0);
-  b.init(B, n0);
-  a.copy(A, m0, k0, lds);
-  b.copy(B, n0, k0, lds + OA::BYTES);
-  __syncthreads();
-  Frags<C, AKC, BKC> f0, f1;
-  f0.read(lds, lds + OA::BYTES, um, un, 0);
-  int buf = 0, k = k0;
-  for (; k + OA::BK < k1; k += OA::BK) {
-    const lds_u8* now = lds + buf * HALF;
-    lds_u8* next = lds + (buf ^ 1) * HALF;
-    f1.read(now, now + OA::BYTES, um, un, 1);
-    a.copy(A, m0, k + OA::BK, next);
-    b.copy(B, n0, k + OA::BK, next + OA::BYTES);
-    f0.multiply(acc, 0, C::MT);
-    f1.multiply(acc, 0, EARLY);
-    interleave<0x100, READS, 1>();
-    interleave<0x010, OA::NL + OB::NL, 1>();
-    __builtin_amdgcn_sched_barrier(0);
-    __syncthreads();
-    f0.read(next, next + OA::BYTES, um, un, 0);
-    f1.multiply(acc, EARLY, C::MT);
-    interleave<0x100, READS, ((C::MT - EARLY) * MUL + READS - 1) / READS>();
-    __builtin_amdgcn_sched_barrier(0);
-    buf ^= 1;
-  }
-  f1.read(lds + buf * HALF, lds + buf * HALF + OA::BYTES, um, un, 1);
-  f0.multiply(acc, 0, C::MT);
-  f1.multiply(acc, 0, C::MT);
+  Product<C, AKC, BKC> p{A, B, uniform(m0), uniform(n0), uniform(k1 < A.k ? (k1 < B.k ? k1 : B.k) : (A.k < B.k ? A.k : B.k)),
+                         fragment_place<typename C::T, C::BM, AKC>((wave % C::WM) * 16 * C::MT),
+                         fragment_place<typename C::T, C::BN, BKC>((wave / C::WM) * 16 * C::NT)};
+  p.run(uniform(k0), lds, acc);
 }
 
 // Order of the tiles of a launch: workgroup i runs on XCD i mod 8, which gets a run of neighbouring tiles, eight along n for each
@@ -389,7 +427,7 @@ __device__ __forceinline__ Src vocab_rows(const HeadDev& h, int64_t first, int64
 template <class C>
 __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_kernel(HeadDev h, int mt) {
   typedef typename C::T T;
-  __shared__ __attribute__((aligned(128))) unsigned char smem[C::LDS];
+  HEAD_BUFFERS
   const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
   const int nt = (n + C::BN - 1) / C::BN;
   if ((int)blockIdx.x >= mt * nt) return;
@@ -397,7 +435,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_
   place_tile(blockIdx.x, mt, nt, tm, tn);
   const int m0 = tm * C::BM, n0 = tn * C::BN;
   Acc<C> acc;
-  product<C, true, true>(vocab_rows<T>(h, 0, h.vocab), packed_x<T>(h, n), m0, n0, 0, h.cols, (lds_u8*)smem, acc);
+  product<C, true, true>(vocab_rows<T>(h, 0, h.vocab), packed_x<T>(h, n), m0, n0, 0, h.cols, lds, acc);
   HEAD_LANE
   const int* target = reinterpret_cast<const int*>(h.ws + h.lay.target);
   float2* part = reinterpret_cast<float2*>(h.ws + h.lay.part) + (int64_t)(tm * C::WM + wave % C::WM) * h.rows;
@@ -517,7 +555,7 @@ __global__ __launch_bounds__(256) void no_rows_dw_kernel(HeadDev h) {
 template <class C>
 __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void piece_kernel(HeadDev h, int64_t first, int width, int64_t pitch, int mt) {
   typedef typename C::T T;
-  __shared__ __attribute__((aligned(128))) unsigned char smem[C::LDS];
+  HEAD_BUFFERS
   const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
   const int nt = (n + C::BN - 1) / C::BN;
   if ((int)blockIdx.x >= mt * nt) return;
@@ -525,7 +563,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void piece_k
   place_tile(blockIdx.x, mt, nt, tm, tn);
   const int m0 = tm * C::BM, n0 = tn * C::BN;
   Acc<C> acc;
-  product<C, true, true>(vocab_rows<T>(h, first, width), packed_x<T>(h, n), m0, n0, 0, h.cols, (lds_u8*)smem, acc);
+  product<C, true, true>(vocab_rows<T>(h, first, width), packed_x<T>(h, n), m0, n0, 0, h.cols, lds, acc);
   HEAD_LANE
   T* P = reinterpret_cast<T*>(h.ws + h.lay.p);
 #pragma unroll
@@ -575,7 +613,7 @@ struct GradPlan {
 template <class C>
 __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_kernel(HeadDev h, GradPlan g) {
   typedef typename C::T T;
-  __shared__ __attribute__((aligned(128))) unsigned char smem[C::LDS];
+  HEAD_BUFFERS
   const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
   const char* P = h.ws + h.lay.p;
   const int64_t pp = g.pitch * (int64_t)sizeof(T);
@@ -587,7 +625,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_ke
     place_tile(blockIdx.x, g.mt, g.nt_w, tm, tn);
     const int m0 = tm * C::BM, n0 = tn * C::BN;
     product<C, false, false>(Src{h.ws + h.lay.x, (int64_t)h.pitch * (int)sizeof(T), h.pitch, n}, Src{P, pp, (int)g.pitch, n}, m0, n0, 0, n,
-                             (lds_u8*)smem, acc);
+                             lds, acc);
     const float f = grad_factor(h, n);
 #pragma unroll
     for (int j = 0; j < C::NT; ++j) {
@@ -627,7 +665,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_ke
   const int cols = W.k;
   W.u = cols;
   W.k = g.width;
-  product<C, false, true>(W, Src{P, pp, n, (int)g.pitch}, m0, n0, k0, k1, (lds_u8*)smem, acc);
+  product<C, false, true>(W, Src{P, pp, n, (int)g.pitch}, m0, n0, k0, k1, lds, acc);
   float* sum = reinterpret_cast<float*>(h.ws + h.lay.acc) + (int64_t)split * h.rows * h.pitch;
 #pragma unroll
   for (int j = 0; j < C::NT; ++j) {

@@ -31,7 +31,7 @@ typedef __attribute__((address_space(3))) unsigned char lds_u8;
 constexpr unsigned OOB = 0x80000000u;                 // an offset past every descriptor's end: reads zeros
 constexpr int64_t PIECE_BYTES = (int64_t)128 << 20;   // most of P at a time: half of what the last-level cache holds
 constexpr float LOG2E = 1.44269504088896340736f;
-constexpr float LN2 = 0.69314718055994530942f;
+constexpr float LOG2E_LOW = (float)(1.44269504088896340736 - (double)LOG2E);
 
 struct HeadHeader {
   int n;                                              // rows that count
@@ -441,6 +441,17 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_
   float2* part = reinterpret_cast<float2*>(h.ws + h.lay.part) + (int64_t)(tm * C::WM + wave % C::WM) * h.rows;
   float* hit = reinterpret_cast<float*>(h.ws + h.lay.hit);
   const int v0 = m0 + um + 4 * q;
+  // columns behind the vocabulary's end, in its last tile
+  if (m0 + C::BM > h.vocab) {
+#pragma unroll
+    for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v0 + 16 * i + e >= h.vocab) {
+#pragma unroll
+          for (int j = 0; j < C::NT; ++j) acc.v[i][j][e] = -INFINITY;
+        }
+  }
 #pragma unroll
   for (int j = 0; j < C::NT; ++j) {
     const int row = n0 + un + 16 * j + l16;
@@ -448,20 +459,20 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_
 #pragma unroll
     for (int i = 0; i < C::MT; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (v0 + 16 * i + e < h.vocab) top = fmaxf(top, acc.v[i][j][e]);
+      for (int e = 0; e < 4; ++e) top = fmaxf(top, acc.v[i][j][e]);
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    // a wave without a column of the vocabulary leaves (-inf, 0)
-    const float shift = top == -INFINITY ? 0.f : top;
+    // exp(s - top) = 2^(s log2 e - c) 2^-rest with c = top log2 e rounded: one multiply-add an element, and what the rounding of c has
+    // left out goes into the sum once.  A wave without a column of the vocabulary leaves (-inf, 0).
+    const float c = top == -INFINITY ? 0.f : top * LOG2E, rest = top == -INFINITY ? 0.f : fmaf(top, LOG2E, -c) + top * LOG2E_LOW;
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < C::MT; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (v0 + 16 * i + e < h.vocab) sum += __builtin_amdgcn_exp2f((acc.v[i][j][e] - shift) * LOG2E);
+      for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc.v[i][j][e], LOG2E, -c));
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
+    sum *= __builtin_amdgcn_exp2f(-rest);
     if (row < n) {
       if (q == 0) part[row] = make_float2(top, sum);
       const int rel = target[row] - v0;
@@ -570,28 +581,44 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void piece_k
   for (int j = 0; j < C::NT; ++j) {
     const int row = n0 + un + 16 * j + l16;
     if (row >= n) continue;
-    const int target = reinterpret_cast<const int*>(h.ws + h.lay.target)[row] - (int)first;
+    const int target = reinterpret_cast<const int*>(h.ws + h.lay.target)[row] - (int)first - (m0 + um + 4 * q);
     const float weight = reinterpret_cast<const float*>(h.ws + h.lay.weight)[row];
-    const float lse = reinterpret_cast<const float*>(h.ws + h.lay.lse)[row];
+    const float lse = reinterpret_cast<const float*>(h.ws + h.lay.lse)[row], lse2 = lse * LOG2E;
+    f32x4 p[C::MT];
+#pragma unroll
+    for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        // fp32: the accurate exponential; bf16 rounds P to 8 bits (the matrix cores' operand), the hardware's is far inside that
+        p[i][e] = sizeof(T) == 4 ? expf(acc.v[i][j][e] - lse) : __builtin_amdgcn_exp2f(fmaf(acc.v[i][j][e], LOG2E, -lse2));
+    if (target >= 0 && target < 16 * C::MT) {        // few lanes ever
+#pragma unroll
+      for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[i][e] -= target == 16 * i + e ? 1.f : 0.f;
+    }
+    if (h.row_weight) {
+#pragma unroll
+      for (int i = 0; i < C::MT; ++i) p[i] *= weight;
+    }
+    if (m0 + C::BM > width) {                        // the piece's last tile: zeros up to its pitch
+#pragma unroll
+      for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[i][e] = m0 + um + 16 * i + 4 * q + e < width ? p[i][e] : 0.f;
+    }
 #pragma unroll
     for (int i = 0; i < C::MT; ++i) {
       const int v = m0 + um + 16 * i + 4 * q;
-      float p[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        // fp32: the accurate exponential; bf16 rounds P to 8 bits (the matrix cores' operand), the hardware's is far inside that
-        const float x = sizeof(T) == 4 ? expf(acc.v[i][j][e] - lse) : __builtin_amdgcn_exp2f((acc.v[i][j][e] - lse) * LOG2E);
-        p[e] = v + e < width ? weight * (x - (v + e == target ? 1.f : 0.f)) : 0.f;
-      }
       T* to = P + (int64_t)row * pitch + v;
       if (v < pitch) {
         if (sizeof(T) == 2) {
           u32x2 w;
-          w[0] = pack_bf16x2(p[0], p[1]);
-          w[1] = pack_bf16x2(p[2], p[3]);
+          w[0] = pack_bf16x2(p[i][0], p[i][1]);
+          w[1] = pack_bf16x2(p[i][2], p[i][3]);
           *reinterpret_cast<u32x2*>(to) = w;
         } else {
-          *reinterpret_cast<f32x4*>(to) = f32x4{p[0], p[1], p[2], p[3]};
+          *reinterpret_cast<f32x4*>(to) = p[i];
         }
       }
     }

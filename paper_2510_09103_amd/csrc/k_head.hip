@@ -15,6 +15,8 @@
 #include "ew_math.h"
 #include "ops_plan.h"
 
+#include <cmath>
+
 namespace adapm {
 
 namespace {
@@ -29,7 +31,7 @@ typedef f32x4 f32x4_e4 __attribute__((aligned(4), may_alias));
 typedef __attribute__((address_space(3))) unsigned char lds_u8;
 
 constexpr unsigned OOB = 0x80000000u;                 // an offset past every descriptor's end: reads zeros
-constexpr int64_t PIECE_BYTES = (int64_t)128 << 20;   // most of P at a time: half of what the last-level cache holds
+constexpr int64_t PIECE_BYTES = (int64_t)256 << 20;   // most of P at a time: the size of the last-level cache
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr float LOG2E_LOW = (float)(1.44269504088896340736 - (double)LOG2E);
 
@@ -633,10 +635,10 @@ struct GradPlan {
   int splits, k_split;    // dx: parts of the contraction and their length
   int nt_w;               // dW: tiles along the vocabulary
   int begin;              // first piece: dx's sums are written, not added to
+  int first_dw;           // workgroups [first_dw, first_dw + mt nt_w) make dW
 };
 
-// backward of a piece: workgroups [0, mt nt_w) make dW (m = columns, n = vocabulary, k = rows of x), the others dx (m = columns, n =
-// rows of x, k = the piece's vocabulary)
+// backward of a piece: dW (m = columns, n = vocabulary, k = rows of x) and dx (m = columns, n = rows of x, k = the piece's vocabulary)
 template <class C>
 __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_kernel(HeadDev h, GradPlan g) {
   typedef typename C::T T;
@@ -647,9 +649,10 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_ke
   const int n_dw = g.mt * g.nt_w;
   HEAD_LANE
   Acc<C> acc;
-  if ((int)blockIdx.x < n_dw) {
+  const int dw_id = (int)blockIdx.x - g.first_dw;
+  if (dw_id >= 0 && dw_id < n_dw) {
     int tm, tn;
-    place_tile(blockIdx.x, g.mt, g.nt_w, tm, tn);
+    place_tile(dw_id, g.mt, g.nt_w, tm, tn);
     const int m0 = tm * C::BM, n0 = tn * C::BN;
     product<C, false, false>(Src{h.ws + h.lay.x, (int64_t)h.pitch * (int)sizeof(T), h.pitch, n}, Src{P, pp, (int)g.pitch, n}, m0, n0, 0, n,
                              lds, acc);
@@ -681,7 +684,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_ke
     }
     return;
   }
-  const int nt = (n + C::BN - 1) / C::BN, per = g.mt * nt, id = (int)blockIdx.x - n_dw;
+  const int nt = (n + C::BN - 1) / C::BN, per = g.mt * nt, id = dw_id < 0 ? (int)blockIdx.x : dw_id - n_dw;
   if (id >= per * g.splits) return;
   const int split = id / per;
   int tm, tn;
@@ -744,20 +747,73 @@ Shape shape_of(int64_t rows, bool bf16) {
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Vocabulary rows of a piece: P of all rows of x fits PIECE_BYTES, but at least 2048 columns of it; pieces of equal width
-int64_t piece_width(int64_t rows, int64_t vocab, bool bf16) {
-  const int64_t fit = PIECE_BYTES / ((bf16 ? 2 : 4) * rows) / 256 * 256;
-  const int64_t most = fit < 2048 ? 2048 : fit;
-  const int64_t pieces = (vocab + most - 1) / most;
-  return up((vocab + pieces - 1) / pieces, 256);
+// How the backward pass is cut.
+struct Cut {
+  int64_t width;      // vocabulary rows of a piece
+  int splits;         // parts of dx's contraction over them
+  bool dx_first;      // dx's tiles are given out before dW's
+};
+
+// Time that `slots` workgroups take for n1 tiles of length l1 and then n2 tiles of length l2, each taking the next one when it is done.
+double finish_time(int64_t n1, double l1, int64_t n2, double l2, int64_t slots) {
+  const int64_t full = n1 / slots, rest = n1 % slots;
+  const double early = (double)full * l1, late = rest ? early + l1 : early;      // when the free and the busy slots are through with n1
+  double end = late;
+  if (n2 > 0) {
+    // tiles done by the time t: (slots - rest) floor((t - early) / l2) + rest floor((t - late) / l2)
+    const double even = ((double)n2 * l2 + (double)(slots - rest) * early + (double)rest * late) / (double)slots;
+    for (double t = even > early + l2 ? even : early + l2;; t += 0.25 * l2) {
+      const double done = (double)(slots - rest) * std::floor((t - early) / l2 + 1e-9) + (t > late ? (double)rest * std::floor((t - late) / l2 + 1e-9) : 0.0);
+      if (done >= (double)n2) {
+        end = end > t ? end : t;
+        break;
+      }
+    }
+  }
+  return end;
 }
 
-// dx has few tiles where there are few rows: its contraction is cut until the launch has a workgroup for every compute unit
-int dx_splits(int64_t rows, int64_t width, int64_t cols, const Shape& f) {
-  const int64_t tiles = ((rows + f.bn - 1) / f.bn) * ((cols + f.bm - 1) / f.bm);
-  int64_t s = (256 + tiles - 1) / tiles;
-  const int64_t most = (width + 255) / 256;
-  return (int)(s < 1 ? 1 : s > most ? most : s);
+// The tiles of a piece's gradients are few and unequal: those of dW have the rows of x for their contraction, those of dx the piece's
+// vocabulary, which can be cut, at the price of one more fp32 sum of dx to write and read.  Pieces of equal width, the parts of dx and
+// which tiles come first are chosen by the time that follows from the tiles, in slices (a tile's beginning and end cost about TILE
+// of them), for all rows and for two thirds of them: how many count is known on the device alone.  Loss and gradients of 8192 rows over
+// 32000 x 2048 / of 5500 over 32000 x 512, in four pieces of 134 MB 3527 / 1053 us (2 x 32 tiles of dW leave half of the chip idle in the
+// second), in three 3905 / 947, in two 3519 / 899, in one that the last-level cache does not hold 3606 / 872.
+Cut cut_of(int64_t rows, int64_t vocab, int64_t cols, bool bf16, const Shape& f, bool want_dx) {
+  constexpr double TILE = 4.0;
+  const int64_t es = bf16 ? 2 : 4, bk = 128 / es, slots = f.big ? 256 : bf16 ? 768 : 512;
+  const double slice_bytes = f.big ? 6e6 : bf16 ? 1.5e6 : 12e6;       // of memory traffic in the time of a slice of all slots
+  int64_t fewest = (rows * vocab * es + PIECE_BYTES - 1) / PIECE_BYTES;
+  const int64_t most = (vocab + 2047) / 2048;                         // pieces of at least 2048
+  if (fewest > most) fewest = most;
+  const int64_t mt = (cols + f.bm - 1) / f.bm, kd = (cols + bk - 1) / bk;
+  Cut best{0, 1, false};
+  double least = 0.0;
+  for (int64_t p = fewest; p <= most && p <= 4 * fewest; p += (fewest + 1) / 2) {
+    const int64_t width = up((vocab + p - 1) / p, 256), pieces = (vocab + width - 1) / width;
+    const int64_t mp = (width + f.bm - 1) / f.bm, tw = mt * ((width + f.bn - 1) / f.bn), kv = width / bk;
+    static const int parts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
+    for (int sp : parts) {
+      if (sp > 1 && (!want_dx || sp * 256 > width)) break;
+      const double lx = (double)((kv + sp - 1) / sp) + TILE;
+      for (int dx_first = 0; dx_first < (want_dx ? 2 : 1); ++dx_first) {
+        double t = 0.0;
+        for (int64_t n = rows; n >= rows * 2 / 3 && n > 0; n = n == rows && rows > 2 ? rows * 2 / 3 : 0) {
+          const int64_t nt = (n + f.bn - 1) / f.bn, tx = want_dx ? mt * nt * sp : 0;
+          const double lw = (double)((n + bk - 1) / bk) + TILE;
+          t += finish_time(mp * nt, (double)kd + TILE, 0, 1.0, slots) +
+               (dx_first ? finish_time(tx, lx, tw, lw, slots) : finish_time(tw, lw, tx, lx, slots)) +
+               (want_dx ? 8.0 * (double)n * (double)cols * sp / slice_bytes : 0.0);
+        }
+        t *= (double)pieces;
+        if (best.width == 0 || t < least) {
+          best = Cut{width, sp, dx_first != 0};
+          least = t;
+        }
+      }
+    }
+  }
+  return best;
 }
 
 template <class C>
@@ -780,6 +836,7 @@ void gradients(const HeadDev& h, int64_t width, int splits, hipStream_t s) {
     g.k_split = (int)up((g.width + splits - 1) / splits, 64);
     g.nt_w = h.dw.p ? (g.width + C::BN - 1) / C::BN : 0;
     g.begin = first == 0;
+    g.first_dw = h.lay.dx_first && h.dx.p ? g.mt * np * g.splits : 0;
     hipLaunchKernelGGL((grad_kernel<C>), dim3((unsigned)(g.mt * (g.nt_w + np * g.splits))), dim3(C::THREADS), 0, s, h, g);
   }
 }
@@ -803,6 +860,9 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, boo
   const int64_t es = bf16 ? 2 : 4, pitch = up(cols, bf16 ? 64 : 32);
   const Shape f = shape_of(rows, bf16);
   HeadLayout l;
+  l.width = 0;
+  l.splits = 0;
+  l.dx_first = false;
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t o = at;
@@ -824,9 +884,12 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, boo
     l.hit = take(4 * rows);
     l.sums = take(8 * ((rows + 63) / 64));
   } else {
-    const int64_t width = piece_width(rows > 0 ? rows : 1, vocab, bf16);
-    l.p = take(rows * width * es);
-    if (want_dx) l.acc = take(4 * rows * pitch * dx_splits(rows > 0 ? rows : 1, width, cols, f));
+    const Cut c = cut_of(rows > 0 ? rows : 1, vocab, cols, bf16, f, want_dx);
+    l.width = c.width;
+    l.splits = c.splits;
+    l.dx_first = c.dx_first;
+    l.p = take(rows * c.width * es);
+    if (want_dx) l.acc = take(4 * rows * pitch * c.splits);
   }
   l.bytes = at;
   return l;
@@ -857,8 +920,8 @@ void launch_head_backward(const HeadDev& h, hipStream_t s) {
   }
   pack(h, s);
   const Shape f = shape_of(h.rows, h.bf16);
-  const int64_t width = piece_width(h.rows, h.vocab, h.bf16);
-  const int splits = dx_splits(h.rows, width, h.cols, f);
+  const int64_t width = h.lay.width;
+  const int splits = h.lay.splits;
   if (!h.bf16) gradients<F32>(h, width, splits, s);
   else if (f.big) gradients<Big>(h, width, splits, s);
   else gradients<Small>(h, width, splits, s);

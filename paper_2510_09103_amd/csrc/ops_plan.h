@@ -52,6 +52,9 @@ struct HeadLayout {
   int64_t x, w;                                               // packed x [rows][pitch], packed W [vocab][pitch]
   int64_t part, hit, sums;                                    // forward: maxima and sums of the tiles, target logits, loss sums
   int64_t p, acc;                                             // backward: a piece of P, sums of dx
+  int64_t width;                                              // ... vocabulary rows of a piece
+  int splits;                                                 // ... parts of dx's contraction over them
+  bool dx_first;                                              // ... dx's tiles are given out before dW's
   int64_t bytes;
 };
 

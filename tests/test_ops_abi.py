@@ -119,7 +119,7 @@ def test_workspace_sizes():
     w = B.rows(A, 1024)
     fwd, bwd = (B.adapm_head_workspace_bytes(big, w, b) for b in (False, True))
     x = 8192 * 1024 * 2
-    assert x < fwd < x + 8 * 8192 * 800 and bwd < 2 * x + (128 << 20) + 4 * 8192 * 1024 * 2
+    assert x < fwd < x + 8 * 8192 * 800 and bwd < 2 * x + (256 << 20) + 4 * 8192 * 1024 * 8
     # rows of W that are no whole vectors are copied
     odd = B.adapm_head_workspace_bytes(big, B.rows(A, 1025), True)
     assert odd >= bwd + 50304 * 1024 * 2

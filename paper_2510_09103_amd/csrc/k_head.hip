@@ -178,9 +178,9 @@ struct Operand {
   // Where a piece stands.  KC: its place among the eight of its row is exchanged by the row's number.  Else pieces of 32 bytes (bf16; a
   // read touches rows 0 .. 3 and 8 .. 11 of a step at a time) or 64 bytes (fp32; rows 0, 4, 8 and 12) are exchanged by the row, over the
   // 256 bytes of all banks: where an LDS row is 128 bytes, its number's lowest bit says which half it lies in already.
-  static_assert(KC || (ES == 2 && BU * ES == 128) || BU * ES >= 256, "exchanged inside a row");
+  static_assert(KC || BU * ES == 128 || BU * ES >= 256, "exchanged inside a row");
   static __device__ __forceinline__ int swz(int k) {
-    if (ES == 4) return (k >> 2) & 3;
+    if (ES == 4) return BU * ES == 128 ? (k >> 2) & 1 : (k >> 2) & 3;        // 128 bytes: two of the four rows share banks
     return BU * ES == 128 ? ((k >> 1) & 1) | ((k >> 2) & 2) : (k & 3) | ((k >> 1) & 4);
   }
 
@@ -491,8 +491,8 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_
 }
 
 // Joins the tiles' maxima and sums: RL rows a workgroup, whose 1024 / RL slices share the tiles; each row's loss, and the workgroup's
-// sum of them.  Up to 8 rows take 128 slices (one row over 32000 columns: 28.5 us with 16 of them, a chain of 63 loads), more rows
-// 16, whose loads are whole lines.
+// sum of them.  RL = 8, 128 slices (one row over 32000 columns: 28.5 us with 16 of them, a chain of 63 loads) up to 2048 rows, which fill
+// the chip with such workgroups; beyond, RL = 64 and 16 slices, whose loads are whole lines.
 template <int RL>
 __global__ __launch_bounds__(1024) void finish_kernel(HeadDev h, int tiles, int last) {
   constexpr int SL = 1024 / RL;
@@ -731,27 +731,34 @@ __global__ __launch_bounds__(256) void dx_kernel(HeadDev h, int splits) {
 }
 
 // ---- plans ------------------------------------------------------------------------------------------------------------
+// Tiles: vocabulary or columns x rows (dW: columns x vocabulary)
 typedef Cfg<uint16_t, 8, 4, 2, 4> Big;        // 256 x 256, eight wavefronts
 typedef Cfg<uint16_t, 2, 4, 4, 1> Small;      // 128 x 64, four
-typedef Cfg<float, 4, 4, 2, 2> F32;           // 128 x 128, four
+typedef Cfg<float, 4, 4, 2, 2> Big32;         // 128 x 128, four
+typedef Cfg<float, 2, 2, 4, 1> Small32;       // 128 x 32, four
 
+// A kind of tile, how many workgroups run at a time, and what a slice of one takes then
 struct Shape {
-  bool big;
-  int bm, bn, wm;
+  int kind, bm, bn, wm;
+  int64_t slots;
+  double slice_us;
 };
-Shape shape_of(int64_t rows, bool bf16) {
-  if (!bf16) return {false, F32::BM, F32::BN, F32::WM};
-  if (rows > 128) return {true, Big::BM, Big::BN, Big::WM};
-  return {false, Small::BM, Small::BN, Small::WM};
+template <class C>
+constexpr Shape shape(int kind, int per_cu, double slice_us) {
+  return Shape{kind, C::BM, C::BN, C::WM, 256 * per_cu, slice_us};
 }
+constexpr Shape SHAPES[4] = {shape<Big>(0, 1, 1.57), shape<Small>(1, 3, 0.85), shape<Big32>(2, 2, 3.9), shape<Small32>(3, 4, 2.3)};
+constexpr double TILE = 4.0;                  // a tile's beginning and end, in slices
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // How the backward pass is cut.
 struct Cut {
+  const Shape* shape;
   int64_t width;      // vocabulary rows of a piece
   int splits;         // parts of dx's contraction over them
   bool dx_first;      // dx's tiles are given out before dW's
+  double us;          // what it should take
 };
 
 // Time that `slots` workgroups take for n1 tiles of length l1 and then n2 tiles of length l2, each taking the next one when it is done.
@@ -775,20 +782,17 @@ double finish_time(int64_t n1, double l1, int64_t n2, double l2, int64_t slots) 
 
 // The tiles of a piece's gradients are few and unequal: those of dW have the rows of x for their contraction, those of dx the piece's
 // vocabulary, which can be cut, at the price of one more fp32 sum of dx to write and read.  Pieces of equal width, the parts of dx and
-// which tiles come first are chosen by the time that follows from the tiles, in slices (a tile's beginning and end cost about TILE
-// of them), for all rows and for two thirds of them: how many count is known on the device alone.  Loss and gradients of 8192 rows over
+// which tiles come first are chosen by the time that follows from the tiles, for all rows and for two thirds of them: how many count is known on the device alone.  Loss and gradients of 8192 rows over
 // 32000 x 2048 / of 5500 over 32000 x 512, in four pieces of 134 MB 3527 / 1053 us (2 x 32 tiles of dW leave half of the chip idle in the
 // second), in three 3905 / 947, in two 3519 / 899, in one that the last-level cache does not hold 3606 / 872.
-Cut cut_of(int64_t rows, int64_t vocab, int64_t cols, bool bf16, const Shape& f, bool want_dx) {
-  constexpr double TILE = 4.0;
-  const int64_t es = bf16 ? 2 : 4, bk = 128 / es, slots = f.big ? 256 : bf16 ? 768 : 512;
-  const double slice_bytes = f.big ? 6e6 : bf16 ? 1.5e6 : 12e6;       // of memory traffic in the time of a slice of all slots
+Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, const Shape& f, bool want_dx) {
+  const int64_t es = bf16 ? 2 : 4, bk = 128 / es, slots = f.slots;
+  const double slice_bytes = 4e6 * f.slice_us;                        // of memory traffic in the time of a slice
   int64_t fewest = (rows * vocab * es + PIECE_BYTES - 1) / PIECE_BYTES;
   const int64_t most = (vocab + 2047) / 2048;                         // pieces of at least 2048
   if (fewest > most) fewest = most;
   const int64_t mt = (cols + f.bm - 1) / f.bm, kd = (cols + bk - 1) / bk;
-  Cut best{0, 1, false};
-  double least = 0.0;
+  Cut best{&f, 0, 1, false, 0.0};
   for (int64_t p = fewest; p <= most && p <= 4 * fewest; p += (fewest + 1) / 2) {
     const int64_t width = up((vocab + p - 1) / p, 256), pieces = (vocab + width - 1) / width;
     const int64_t mp = (width + f.bm - 1) / f.bm, tw = mt * ((width + f.bn - 1) / f.bn), kv = width / bk;
@@ -805,15 +809,42 @@ Cut cut_of(int64_t rows, int64_t vocab, int64_t cols, bool bf16, const Shape& f,
                (dx_first ? finish_time(tx, lx, tw, lw, slots) : finish_time(tw, lw, tx, lx, slots)) +
                (want_dx ? 8.0 * (double)n * (double)cols * sp / slice_bytes : 0.0);
         }
-        t *= (double)pieces;
-        if (best.width == 0 || t < least) {
-          best = Cut{width, sp, dx_first != 0};
-          least = t;
-        }
+        t *= (double)pieces * f.slice_us;
+        if (best.width == 0 || t < best.us) best = Cut{&f, width, sp, dx_first != 0, t};
       }
     }
   }
   return best;
+}
+
+// Which tiles the passes take: those with the shorter time.  bf16 over 50257 x 1600, small and big tiles, us forward / backward: 64 rows 50 /
+// 150 and 54 / 206, 128 rows 65 / 175 and 58 / 202, 256 rows 85 / 253 and 59 / 230, 1024 rows 218 / 693 and 173 / 568; over 4099 x 256,
+// where big tiles are few, 1024 rows 29 / 40 and 30 / 63.
+const Shape& forward_shape(int64_t rows, int64_t vocab, int64_t cols, bool bf16) {
+  const Shape* two = SHAPES + (bf16 ? 0 : 2);
+  double us[2];
+  for (int i = 0; i < 2; ++i) {
+    const Shape& f = two[i];
+    const int64_t tiles = ((vocab + f.bm - 1) / f.bm) * ((rows + f.bn - 1) / f.bn), bk = bf16 ? 64 : 32;
+    us[i] = finish_time(tiles, (double)((cols + bk - 1) / bk) + TILE, 0, 1.0, f.slots) * f.slice_us;
+  }
+  return two[us[1] < us[0] ? 1 : 0];
+}
+
+// The cut depends on the sizes alone and takes some microseconds of the host to find: a thread keeps the last one.
+Cut cut_of(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool want_dx) {
+  struct Last {
+    int64_t rows, vocab, cols;
+    bool bf16, want_dx;
+    Cut cut;
+  };
+  static thread_local Last last{-1, 0, 0, false, false, Cut{nullptr, 0, 1, false, 0.0}};
+  if (last.rows != rows || last.vocab != vocab || last.cols != cols || last.bf16 != bf16 || last.want_dx != want_dx) {
+    const Shape* two = SHAPES + (bf16 ? 0 : 2);
+    const Cut a = cut_with(rows, vocab, cols, bf16, two[0], want_dx), b = cut_with(rows, vocab, cols, bf16, two[1], want_dx);
+    last = Last{rows, vocab, cols, bf16, want_dx, b.us < a.us ? b : a};
+  }
+  return last.cut;
 }
 
 template <class C>
@@ -858,11 +889,11 @@ void pack(const HeadDev& h, hipStream_t s) {
 
 HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx) {
   const int64_t es = bf16 ? 2 : 4, pitch = up(cols, bf16 ? 64 : 32);
-  const Shape f = shape_of(rows, bf16);
   HeadLayout l;
   l.width = 0;
   l.splits = 0;
   l.dx_first = false;
+  l.kind = 0;
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t o = at;
@@ -880,11 +911,15 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, boo
   l.w = w_packed ? take(vocab * pitch * es) : -1;
   l.part = l.hit = l.sums = l.p = l.acc = -1;
   if (!backward) {
-    l.part = take(8 * rows * ((vocab + f.bm - 1) / f.bm) * f.wm);
+    const Shape& f = forward_shape(rows > 0 ? rows : 1, vocab, cols, bf16);
+    l.kind = f.kind;
+    l.tiles = (int)((vocab + f.bm - 1) / f.bm) * f.wm;
+    l.part = take(8 * rows * l.tiles);
     l.hit = take(4 * rows);
-    l.sums = take(8 * ((rows + 63) / 64));
+    l.sums = take(8 * ((rows + 7) / 8));
   } else {
-    const Cut c = cut_of(rows > 0 ? rows : 1, vocab, cols, bf16, f, want_dx);
+    const Cut c = cut_of(rows > 0 ? rows : 1, vocab, cols, bf16, want_dx);
+    l.kind = c.shape->kind;
     l.width = c.width;
     l.splits = c.splits;
     l.dx_first = c.dx_first;
@@ -901,13 +936,15 @@ void launch_head_loss(const HeadDev& h, hipStream_t s) {
     return;
   }
   pack(h, s);
-  const Shape f = shape_of(h.rows, h.bf16);
-  if (!h.bf16) logits<F32>(h, s);
-  else if (f.big) logits<Big>(h, s);
-  else logits<Small>(h, s);
-  const int tiles = (int)((h.vocab + f.bm - 1) / f.bm) * f.wm, groups = (int)((h.rows + 63) / 64);
-  if (h.rows <= 8) hipLaunchKernelGGL((finish_kernel<8>), dim3(1), dim3(1024), 0, s, h, tiles, 1);
-  else hipLaunchKernelGGL((finish_kernel<64>), dim3((unsigned)groups), dim3(1024), 0, s, h, tiles, groups == 1 ? 1 : 0);
+  switch (h.lay.kind) {
+    case 0: logits<Big>(h, s); break;
+    case 1: logits<Small>(h, s); break;
+    case 2: logits<Big32>(h, s); break;
+    default: logits<Small32>(h, s); break;
+  }
+  const int tiles = h.lay.tiles, rl = h.rows <= 2048 ? 8 : 64, groups = (int)((h.rows + rl - 1) / rl);
+  if (rl == 8) hipLaunchKernelGGL((finish_kernel<8>), dim3((unsigned)groups), dim3(1024), 0, s, h, tiles, groups == 1 ? 1 : 0);
+  else hipLaunchKernelGGL((finish_kernel<64>), dim3((unsigned)groups), dim3(1024), 0, s, h, tiles, 0);
   if (groups > 1) hipLaunchKernelGGL(total_kernel, dim3(1), dim3(256), 0, s, h, groups);
 }
 
@@ -919,12 +956,14 @@ void launch_head_backward(const HeadDev& h, hipStream_t s) {
     return;
   }
   pack(h, s);
-  const Shape f = shape_of(h.rows, h.bf16);
   const int64_t width = h.lay.width;
   const int splits = h.lay.splits;
-  if (!h.bf16) gradients<F32>(h, width, splits, s);
-  else if (f.big) gradients<Big>(h, width, splits, s);
-  else gradients<Small>(h, width, splits, s);
+  switch (h.lay.kind) {
+    case 0: gradients<Big>(h, width, splits, s); break;
+    case 1: gradients<Small>(h, width, splits, s); break;
+    case 2: gradients<Big32>(h, width, splits, s); break;
+    default: gradients<Small32>(h, width, splits, s); break;
+  }
   if (h.dx.p) {
     if (h.bf16) hipLaunchKernelGGL((dx_kernel<uint16_t>), dim3((unsigned)h.rows), dim3(256), 0, s, h, splits);
     else hipLaunchKernelGGL((dx_kernel<float>), dim3((unsigned)h.rows), dim3(256), 0, s, h, splits);

@@ -50,7 +50,9 @@ void launch_norm_backward(bool bf16, const NormDev& n, hipStream_t s);
 struct HeadLayout {
   int64_t head, counts, list, place, target, weight, lse;     // the rows that count (HeadHeader; int32 / float [rows])
   int64_t x, w;                                               // packed x [rows][pitch], packed W [vocab][pitch]
+  int kind;                                                   // which tiles the products take
   int64_t part, hit, sums;                                    // forward: maxima and sums of the tiles, target logits, loss sums
+  int tiles;                                                  // ... of which each row has so many
   int64_t p, acc;                                             // backward: a piece of P, sums of dx
   int64_t width;                                              // ... vocabulary rows of a piece
   int splits;                                                 // ... parts of dx's contraction over them

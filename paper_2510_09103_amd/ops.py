@@ -40,26 +40,41 @@ class Loss(NamedTuple):
     lse: torch.Tensor                    # fp32, one a row
 
 
-def _matrix(name, t, like=None, dtype=None, shape=None):
-    """t as a matrix of rows: any number of leading dimensions whose rows are evenly spaced; (tensor, rows, cols, stride)."""
+def _first(name, t):
+    """The tensor that gives a call its device, type and shape: (its matrix, rows, columns)."""
     if not isinstance(t, torch.Tensor) or t.dim() < 1:
         raise ValueError(f"{name}: a tensor with at least one dimension is wanted")
     if t.device.type != "cuda":
         raise ValueError(f"{name}: on {t.device}, a GPU tensor is wanted")
-    if like is not None and t.device != like.device:
-        raise ValueError(f"{name}: on {t.device}, the other tensors are on {like.device}")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{name}: {t.dtype}, {dtype} is wanted")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, {tuple(shape)} is wanted")
     cols = t.shape[-1]
     if cols == 0:
         raise ValueError(f"{name}: rows of no elements")
+    return B.adapm_rows_t(t.data_ptr(), cols if t.is_contiguous() else _stride(name, t)), t.numel() // cols, cols
+
+
+def _rows(name, t, like, dtype, shape):
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name}: on {t.device}, the other tensors are on {like.device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: {t.dtype}, {dtype} is wanted")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, {tuple(shape)} is wanted")
+    return B.adapm_rows_t(t.data_ptr(), t.shape[-1] if t.is_contiguous() else _stride(name, t))
+
+
+def _new(t):
+    """An output of the call's own making, whose elements are adjacent."""
+    return B.adapm_rows_t(t.data_ptr(), t.shape[-1])
+
+
+def _stride(name, t):
+    """Elements from one row to the next of a matrix with any number of leading dimensions, whose rows have to be evenly spaced."""
+    cols = t.shape[-1]
     if cols > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: the elements of a row have to be adjacent (stride {t.stride(-1)})")
-    rows, stride = t.numel() // cols, None
+    stride = None
     for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
-        if n == 1 or rows == 0:
+        if n == 1 or t.numel() == 0:
             continue
         if stride is None:
             stride, width = s, n * s
@@ -71,15 +86,11 @@ def _matrix(name, t, like=None, dtype=None, shape=None):
         stride = cols
     if stride < cols:
         raise ValueError(f"{name}: rows overlap (stride {stride}, {cols} elements)")
-    return rows, cols, stride
-
-
-def _rows(name, t, like=None, dtype=None, shape=None):
-    return B.rows(t.data_ptr(), _matrix(name, t, like, dtype, shape)[2])
+    return stride
 
 
 def _vector(name, t, n, like, dtype):
-    if t.device != like.device:
+    if t.get_device() != like.get_device():
         raise ValueError(f"{name}: on {t.device}, the other tensors are on {like.device}")
     if t.dtype != dtype:
         raise TypeError(f"{name}: {t.dtype}, {dtype} is wanted")
@@ -89,9 +100,11 @@ def _vector(name, t, n, like, dtype):
 
 
 def _float_type(name, t):
-    if t.dtype not in (torch.float32, torch.bfloat16):
-        raise TypeError(f"{name}: {t.dtype}, float32 or bfloat16 is wanted")
-    return _DT[t.dtype]
+    if t.dtype is torch.bfloat16:
+        return B.ADAPM_BF16
+    if t.dtype is torch.float32:
+        return B.ADAPM_F32
+    raise TypeError(f"{name}: {t.dtype}, float32 or bfloat16 is wanted")
 
 
 def _dropout(p, rng, like):
@@ -108,8 +121,16 @@ def _dropout(p, rng, like):
     return B.adapm_dropout_t(rng.seed & mask, rng.offset & mask, at or None, p, 0)
 
 
-def _stream(t):
-    return torch.cuda.current_stream(t.device).cuda_stream
+def _call(f, t, *args):
+    """One library call on t's device and the current stream of that device."""
+    if t.get_device() == torch.cuda.current_device():
+        f(*args, torch.cuda.current_stream(t.device).cuda_stream)
+    else:
+        with torch.cuda.device(t.device):
+            f(*args, torch.cuda.current_stream(t.device).cuda_stream)
+
+
+_NO_ROWS = B.rows()
 
 
 def _scratch(nbytes, like):
@@ -121,13 +142,15 @@ def dropout(x: torch.Tensor, p: float, rng: Rng, residual: Optional[torch.Tensor
             out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """residual + dropout(x), rounded once.  The gradient of x is dropout(gradient of the result, p, rng).  out may be x or residual."""
     dt = _float_type("x", x)
-    n, cols, _ = _matrix("x", x)
+    xr, n, cols = _first("x", x)
+    res = _NO_ROWS if residual is None else _rows("residual", residual, x, x.dtype, x.shape)
+    drop = _dropout(p, rng, x) or B.adapm_dropout_t(0, 0, None, 0.0, 0)
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    res = B.rows() if residual is None else _rows("residual", residual, x, x.dtype, x.shape)
-    drop = _dropout(p, rng, x) or B.adapm_dropout_t(0, 0, None, 0.0, 0)
-    with torch.cuda.device(x.device):
-        B.adapm_dropout(_rows("out", out, x, x.dtype, x.shape), _rows("x", x), res, n, cols, dt, drop, _stream(x))
+        y = _new(out)
+    else:
+        y = _rows("out", out, x, x.dtype, x.shape)
+    _call(B.adapm_dropout, x, y, xr, res, n, cols, dt, drop)
     return out
 
 
@@ -136,21 +159,22 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual:
     """h = residual + dropout(x), y = h / sqrt(mean(h^2) + eps) * weight over the last dimension.  out_dtype: that of x, or
     torch.float8_e4m3fn with a scale for each row (y stands for y * scale)."""
     dt, wt = _float_type("x", x), _float_type("weight", weight)
-    n, cols, _ = _matrix("x", x)
+    xr, n, cols = _first("x", x)
     w = _vector("weight", weight, cols, x, weight.dtype)
     out_dtype = x.dtype if out_dtype is None else out_dtype
     if out_dtype not in (x.dtype, torch.float8_e4m3fn):
         raise TypeError(f"out_dtype {out_dtype}: {x.dtype} or torch.float8_e4m3fn is wanted")
     drop = _dropout(p, rng, x)
-    res = B.rows() if residual is None else _rows("residual", residual, x, x.dtype, x.shape)
-    h = x if residual is None and drop is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    res = _NO_ROWS if residual is None else _rows("residual", residual, x, x.dtype, x.shape)
     y = torch.empty(x.shape, dtype=out_dtype, device=x.device)
     rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     scale = torch.empty_like(rstd) if out_dtype == torch.float8_e4m3fn else None
-    desc = B.adapm_norm_t(n, cols, dt, wt, _DT[out_dtype], wt, eps, 0)
-    with torch.cuda.device(x.device):
-        B.adapm_norm_forward(desc, _rows("x", x), res, B.rows() if h is x else _rows("h", h), w, _rows("y", y),
-                             0 if scale is None else scale.data_ptr(), rstd.data_ptr(), drop, _stream(x))
+    h, hr = x, _NO_ROWS
+    if residual is not None or drop is not None:
+        h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        hr = _new(h)
+    _call(B.adapm_norm_forward, x, B.adapm_norm_t(n, cols, dt, wt, _DT[out_dtype], wt, eps, 0), xr, res, hr, w, _new(y),
+          0 if scale is None else scale.data_ptr(), rstd.data_ptr(), drop)
     return Norm(y, h, rstd, scale)
 
 
@@ -161,39 +185,38 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, r
     Without dropout dx and dresidual are one tensor.  dweight is written where it is given (any shape of cols elements, such as a norm
     vector's gradient in a block table); else it is new, in grad_dtype or the type of weight."""
     dt, wt = _float_type("dy", dy), _float_type("weight", weight)
-    n, cols, _ = _matrix("dy", dy)
+    dyr, n, cols = _first("dy", dy)
     w = _vector("weight", weight, cols, dy, weight.dtype)
     r = _vector("rstd", rstd, n, dy, torch.float32)
     drop = _dropout(p, rng, dy)
-    up = B.rows() if dh is None else _rows("dh", dh, dy, dy.dtype, dy.shape)
-    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
-    dres = dx if drop is None else torch.empty_like(dx)
+    up = _NO_ROWS if dh is None else _rows("dh", dh, dy, dy.dtype, dy.shape)
+    hr = _rows("h", h, dy, dy.dtype, dy.shape)
     if dweight is None:
         dweight = torch.empty(weight.shape, dtype=grad_dtype or weight.dtype, device=dy.device)
     elif grad_dtype is not None and dweight.dtype != grad_dtype:
         raise TypeError(f"dweight: {dweight.dtype}, grad_dtype is {grad_dtype}")
     g = _vector("dweight", dweight, cols, dy, dweight.dtype)
     desc = B.adapm_norm_t(n, cols, dt, wt, dt, _float_type("dweight", dweight), 0.0, 0)
+    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
+    dres = dx if drop is None else torch.empty_like(dx)
     ws = _scratch(B.adapm_norm_workspace_bytes(desc), dy)
-    with torch.cuda.device(dy.device):
-        B.adapm_norm_backward(desc, _rows("dy", dy), up, _rows("h", h, dy, dy.dtype, dy.shape), w, r, _rows("dx", dx),
-                              B.rows() if drop is None else _rows("dresidual", dres), g, drop, ws.data_ptr(), _stream(dy))
+    _call(B.adapm_norm_backward, dy, desc, dyr, up, hr, w, r, _new(dx), _NO_ROWS if drop is None else _new(dres), g, drop, ws.data_ptr())
     return dx, dres, dweight
 
 
 def _head(x, weight, targets, row_weight, reduction, scale):
     dt = _float_type("x", x)
-    n, cols, stride = _matrix("x", x)
+    xr, n, cols = _first("x", x)
     if weight.dim() != 2 or weight.shape[1] != cols:
         raise ValueError(f"weight: shape {tuple(weight.shape)}, (vocabulary, {cols}) is wanted")
     if weight.shape[0] == 0:
         raise ValueError("weight: a vocabulary of no entries")
     if reduction not in _REDUCTION:
         raise ValueError(f"reduction {reduction!r}: 'mean' or 'sum' is wanted")
-    w = _rows("weight", weight, x, x.dtype)
+    w = _rows("weight", weight, x, x.dtype, weight.shape)
     t = _vector("targets", targets, n, x, torch.int64)
     rw = 0 if row_weight is None else _vector("row_weight", row_weight, n, x, torch.float32)
-    return B.adapm_head_t(n, weight.shape[0], cols, dt, _REDUCTION[reduction], scale, 0), B.rows(x.data_ptr(), stride), w, t, rw
+    return B.adapm_head_t(n, weight.shape[0], cols, dt, _REDUCTION[reduction], scale, 0), xr, w, t, rw
 
 
 def head_loss(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, row_weight: Optional[torch.Tensor] = None,
@@ -206,8 +229,7 @@ def head_loss(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, row_
     lse = torch.empty_like(row_loss)
     size = B.adapm_head_workspace_bytes(h, w, False)
     ws = _scratch(size, x)
-    with torch.cuda.device(x.device):
-        B.adapm_head_loss(h, xr, w, t, rw, loss.data_ptr(), row_loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), size, _stream(x))
+    _call(B.adapm_head_loss, x, h, xr, w, t, rw, loss.data_ptr(), row_loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), size)
     return Loss(loss, row_loss, lse)
 
 
@@ -226,10 +248,9 @@ def head_backward(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, 
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     if need_dweight and dweight is None:
         dweight = torch.empty(weight.shape, dtype=x.dtype, device=x.device)
-    gx = _rows("dx", dx, x, x.dtype, x.shape) if need_dx else B.rows()
-    gw = _rows("dweight", dweight, x, x.dtype, weight.shape) if need_dweight else B.rows()
+    gx = _rows("dx", dx, x, x.dtype, x.shape) if need_dx else _NO_ROWS
+    gw = _rows("dweight", dweight, x, x.dtype, weight.shape) if need_dweight else _NO_ROWS
     size = B.adapm_head_workspace_bytes(h, w, True)
     ws = _scratch(size, x)
-    with torch.cuda.device(x.device):
-        B.adapm_head_backward(h, xr, w, t, rw, at, up, gx, gw, ws.data_ptr(), size, _stream(x))
+    _call(B.adapm_head_backward, x, h, xr, w, t, rw, at, up, gx, gw, ws.data_ptr(), size)
     return dx if need_dx else None, dweight if need_dweight else None

@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256) void pack_w_kernel(HeadDev h) {
 // ---- matrix products -------------------------------------------------------------------------------------------------
 // A tile of D[m][n] = sum_k A(m, k) B(n, k).  An operand is stored with k along its rows (KC: element (u, k) at u pitch + k) or
 // across them (at k pitch + u).  128-byte slices of the contraction (64 bf16 or 32 fp32 values, two steps of fragments: whole cache lines
-// where k goes along the rows) are copied straight into one of two LDS buffers; which 16-byte piece of a slice a thread fetches is
+// where k goes along the rows) are copied straight into one of two to four LDS buffers; which 16-byte piece of a slice a thread fetches is
 // exchanged (by the LDS row's number) so that the reads of a fragment fall on different banks without padding.
 // bf16: v_mfma_f32_16x16x32, KC fragments are one 16-byte read, the others two transposing reads of 8 bytes.
 // fp32: v_mfma_f32_16x16x4, four of them to a 16-byte read; which k meets which instruction is the same for both operands.
@@ -177,10 +177,11 @@ struct Operand {
   static_assert(NL * 16 * NTHR == BYTES, "whole pieces");
   // Where a piece stands.  KC: its place among the eight of its row is exchanged by the row's number.  Else pieces of 32 bytes (bf16; a
   // read touches rows 0 .. 3 and 8 .. 11 of a step at a time) or 64 bytes (fp32; rows 0, 4, 8 and 12) are exchanged by the row, over the
-  // 256 bytes of all banks: where an LDS row is 128 bytes, its number's lowest bit says which half it lies in already.
-  static_assert(KC || BU * ES == 128 || BU * ES >= 256, "exchanged inside a row");
+  // 256 bytes of all banks: where an LDS row is 128 or 64 bytes, its number's lowest bits say which half or quarter it lies in already.
+  static_assert(KC || (ES == 2 && BU * ES == 64) || BU * ES == 128 || BU * ES >= 256, "exchanged inside a row");
   static __device__ __forceinline__ int swz(int k) {
     if (ES == 4) return BU * ES == 128 ? (k >> 2) & 1 : (k >> 2) & 3;        // 128 bytes: two of the four rows share banks
+    if (BU * ES == 64) return (k >> 3) & 1;
     return BU * ES == 128 ? ((k >> 1) & 1) | ((k >> 2) & 2) : (k & 3) | ((k >> 1) & 4);
   }
 
@@ -269,20 +270,21 @@ __device__ __forceinline__ f32x4 mma(const u32x4& a, const u32x4& b, f32x4 c, co
   return c;
 }
 
-// waves WM x WN, each MT x NT tiles of 16 x 16
-template <class T_, int MT_, int NT_, int WM_, int WN_>
+// waves WM x WN, each MT x NT tiles of 16 x 16, and DEPTH buffers for slices
+template <class T_, int MT_, int NT_, int WM_, int WN_, int DEPTH_ = 2>
 struct Cfg {
   typedef T_ T;
-  static constexpr int MT = MT_, NT = NT_, WM = WM_, WN = WN_;
+  static constexpr int MT = MT_, NT = NT_, WM = WM_, WN = WN_, DEPTH = DEPTH_;
   static constexpr int BM = 16 * MT * WM, BN = 16 * NT * WN, THREADS = 64 * WM * WN;
   static constexpr int SLICE = (BM + BN) * 128;
 };
-// the two buffers, as arrays of their own: the compiler then knows which copies a read has to wait for
-#define HEAD_BUFFERS                                                                                          \
-  __shared__ __attribute__((aligned(128))) unsigned char buffer0[C::SLICE], buffer1[C::SLICE];                \
-  const Buffers lds{(lds_u8*)buffer0, (lds_u8*)buffer1};
+// the buffers, as arrays of their own: the compiler then knows which copies a read has to wait for
+#define HEAD_BUFFERS                                                                                                                   \
+  __shared__ __attribute__((aligned(128))) unsigned char buffer0[C::SLICE], buffer1[C::SLICE], buffer2[C::DEPTH > 2 ? C::SLICE : 16],  \
+      buffer3[C::DEPTH > 3 ? C::SLICE : 16];                                                                                           \
+  const Buffers lds{(lds_u8*)buffer0, (lds_u8*)buffer1, (lds_u8*)buffer2, (lds_u8*)buffer3};
 struct Buffers {
-  lds_u8 *p0, *p1;
+  lds_u8 *p0, *p1, *p2, *p3;
 };
 
 template <class C>
@@ -295,14 +297,15 @@ struct Acc {
 // one half of a phase behind the first: while one multiplies, with priority, the other reads, and the matrix cores are not left waiting
 // for either.  The barriers between the halves of the phases hold them so.  With four wavefronts the workgroups on a compute unit do
 // that for one another by chance.
-// In the first two phases the next slice is copied into the other buffer; before the last multiplication every wavefront has seen its
-// own copies arrive and its last fragments leave the buffer that the next copies go to.
+// In the first two phases the slice DEPTH - 1 further on is copied into the buffer that was used last; before the last multiplication
+// every wavefront has seen its own copies of the next slice arrive and its last fragments leave the buffer that the next copies go to.
 template <class C, bool AKC, bool BKC>
 struct Product {
   typedef typename C::T T;
   typedef Operand<T, C::BM, C::THREADS, AKC> OA;
   typedef Operand<T, C::BN, C::THREADS, BKC> OB;
   static constexpr int BK = OA::BK, HALF = C::MT / 2;
+  static constexpr int COPIES = OA::NL + OB::NL, LEFT = (C::DEPTH - 2) * COPIES;        // LEFT: copies still on their way at that point
   static constexpr bool PAIRED = C::THREADS == 512;
   static_assert(C::MT % 2 == 0, "two halves");
   const Src A, B;
@@ -339,17 +342,17 @@ struct Product {
       for (int j = 0; j < C::NT; ++j) acc.v[half * HALF + i][j] = mma(fa[i], fb[j], acc.v[half * HALF + i][j], (const T*)nullptr);
     if (PAIRED) __builtin_amdgcn_s_setprio(0);
   }
-  // the slice at k in `now`; the next one goes to `next`
-  __device__ __forceinline__ void slice(int k, const lds_u8* __restrict now, lds_u8* __restrict next, Acc<C>& acc) const {
+  // the slice at k in `now`; the one DEPTH - 1 further on goes to `free`
+  __device__ __forceinline__ void slice(int k, const lds_u8* __restrict now, lds_u8* __restrict free, Acc<C>& acc) const {
     u32x4 fa[HALF], fb[C::NT];
     read_b(fb, now, 0);
     read_a(fa, now, 0, 0);
-    a.copy(A, m0, k + BK, k1, next);
+    a.copy(A, m0, k + (C::DEPTH - 1) * BK, k1, free);
     turn();
     multiply(fa, fb, acc, 0);
     turn();
     read_a(fa, now, 1, 0);
-    b.copy(B, n0, k + BK, k1, next + OA::BYTES);
+    b.copy(B, n0, k + (C::DEPTH - 1) * BK, k1, free + OA::BYTES);
     turn();
     multiply(fa, fb, acc, 1);
     turn();
@@ -360,7 +363,7 @@ struct Product {
     turn();
     read_a(fa, now, 1, 1);
     __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
     barrier();
     multiply(fa, fb, acc, 1);
     turn();
@@ -368,19 +371,32 @@ struct Product {
   __device__ __forceinline__ void run(int k0, const Buffers& lds, Acc<C>& acc) {
     a.init(A, m0);
     b.init(B, n0);
-    a.copy(A, m0, k0, k1, lds.p0);
-    b.copy(B, n0, k0, k1, lds.p0 + OA::BYTES);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_u8* const p[4] = {lds.p0, lds.p1, lds.p2, lds.p3};
+#pragma unroll
+    for (int i = 0; i < C::DEPTH - 1; ++i) {
+      a.copy(A, m0, k0 + i * BK, k1, p[i]);
+      b.copy(B, n0, k0 + i * BK, k1, p[i] + OA::BYTES);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
     barrier();
     const bool second = PAIRED && uniform((int)threadIdx.x) >= 256;
     if (second) barrier();
     for (int k = k0;;) {
-      slice(k, lds.p0, lds.p1, acc);
+      slice(k, p[0], p[C::DEPTH - 1], acc);
       if ((k += BK) >= k1) break;
-      slice(k, lds.p1, lds.p0, acc);
+      slice(k, p[1], p[0], acc);
       if ((k += BK) >= k1) break;
+      if (C::DEPTH > 2) {
+        slice(k, p[2], p[1], acc);
+        if ((k += BK) >= k1) break;
+      }
+      if (C::DEPTH > 3) {
+        slice(k, p[3], p[2], acc);
+        if ((k += BK) >= k1) break;
+      }
     }
     if (PAIRED && !second) barrier();
+    if (LEFT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // no copy outlives the workgroup's use of the buffers
   }
 };
 
@@ -734,21 +750,27 @@ __global__ __launch_bounds__(256) void dx_kernel(HeadDev h, int splits) {
 // Tiles: vocabulary or columns x rows (dW: columns x vocabulary)
 typedef Cfg<uint16_t, 8, 4, 2, 4> Big;        // 256 x 256, eight wavefronts
 typedef Cfg<uint16_t, 2, 4, 4, 1> Small;      // 128 x 64, four
+typedef Cfg<uint16_t, 2, 2, 4, 1, 4> Thin;    // 128 x 32, four; three slices on their way: W streams by
 typedef Cfg<float, 4, 4, 2, 2> Big32;         // 128 x 128, four
 typedef Cfg<float, 2, 2, 4, 1> Small32;       // 128 x 32, four
 
-// A kind of tile, how many workgroups run at a time, and what a slice of one takes then
+// A kind of tile: a compute unit runs per_cu workgroups of it and is through with a slice in `share` then; few of them take `lag` more
 struct Shape {
-  int kind, bm, bn, wm;
-  int64_t slots;
-  double slice_us;
+  int kind, bm, bn, wm, per_cu;
+  double share, lag;
 };
 template <class C>
-constexpr Shape shape(int kind, int per_cu, double slice_us) {
-  return Shape{kind, C::BM, C::BN, C::WM, 256 * per_cu, slice_us};
+constexpr Shape shape(int kind, int per_cu, double share, double lag) {
+  return Shape{kind, C::BM, C::BN, C::WM, per_cu, share, lag};
 }
-constexpr Shape SHAPES[4] = {shape<Big>(0, 1, 1.57), shape<Small>(1, 3, 0.85), shape<Big32>(2, 2, 3.9), shape<Small32>(3, 4, 2.3)};
+constexpr int CUS = 256;
 constexpr double TILE = 4.0;                  // a tile's beginning and end, in slices
+constexpr Shape SHAPES[5] = {shape<Big>(0, 1, 1.57, 0.0), shape<Small>(1, 3, 0.285, 0.45), shape<Thin>(2, 2, 0.25, 0.2),
+                             shape<Big32>(3, 2, 1.95, 0.0), shape<Small32>(4, 4, 0.58, 0.0)};
+// Those for a type.  Thin is for the forward pass of rows that are one of its tiles, where reading W is all: one row over 32000 x 2048 33
+// us, 36 with Small; the products of the backward pass gain nothing from it.
+int first_shape(bool bf16) { return bf16 ? 0 : 3; }
+int end_shape(bool bf16, bool thin) { return !bf16 ? 5 : thin ? 3 : 2; }
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
@@ -761,7 +783,7 @@ struct Cut {
   double us;          // what it should take
 };
 
-// Time that `slots` workgroups take for n1 tiles of length l1 and then n2 tiles of length l2, each taking the next one when it is done.
+// Time that `slots` take for n1 tiles of length l1 and then n2 tiles of length l2, each taking the next one when it is done.
 double finish_time(int64_t n1, double l1, int64_t n2, double l2, int64_t slots) {
   const int64_t full = n1 / slots, rest = n1 % slots;
   const double early = (double)full * l1, late = rest ? early + l1 : early;      // when the free and the busy slots are through with n1
@@ -786,8 +808,8 @@ double finish_time(int64_t n1, double l1, int64_t n2, double l2, int64_t slots) 
 // 32000 x 2048 / of 5500 over 32000 x 512, in four pieces of 134 MB 3527 / 1053 us (2 x 32 tiles of dW leave half of the chip idle in the
 // second), in three 3905 / 947, in two 3519 / 899, in one that the last-level cache does not hold 3606 / 872.
 Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, const Shape& f, bool want_dx) {
-  const int64_t es = bf16 ? 2 : 4, bk = 128 / es, slots = f.slots;
-  const double slice_bytes = 4e6 * f.slice_us;                        // of memory traffic in the time of a slice
+  const int64_t es = bf16 ? 2 : 4, bk = 128 / es, slots = CUS * f.per_cu;
+  const double us_per_byte = 1.0 / 4e6;
   int64_t fewest = (rows * vocab * es + PIECE_BYTES - 1) / PIECE_BYTES;
   const int64_t most = (vocab + 2047) / 2048;                         // pieces of at least 2048
   if (fewest > most) fewest = most;
@@ -805,11 +827,11 @@ Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, const Shape& 
         for (int64_t n = rows; n >= rows * 2 / 3 && n > 0; n = n == rows && rows > 2 ? rows * 2 / 3 : 0) {
           const int64_t nt = (n + f.bn - 1) / f.bn, tx = want_dx ? mt * nt * sp : 0;
           const double lw = (double)((n + bk - 1) / bk) + TILE;
-          t += finish_time(mp * nt, (double)kd + TILE, 0, 1.0, slots) +
-               (dx_first ? finish_time(tx, lx, tw, lw, slots) : finish_time(tw, lw, tx, lx, slots)) +
-               (want_dx ? 8.0 * (double)n * (double)cols * sp / slice_bytes : 0.0);
+          t += (finish_time(mp * nt, (double)kd + TILE, 0, 1.0, slots) +
+                (dx_first ? finish_time(tx, lx, tw, lw, slots) : finish_time(tw, lw, tx, lx, slots))) * f.share * f.per_cu +
+               (want_dx ? 8.0 * (double)n * (double)cols * sp * us_per_byte : 0.0);
         }
-        t *= (double)pieces * f.slice_us;
+        t *= (double)pieces;
         if (best.width == 0 || t < best.us) best = Cut{&f, width, sp, dx_first != 0, t};
       }
     }
@@ -821,14 +843,19 @@ Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, const Shape& 
 // 150 and 54 / 206, 128 rows 65 / 175 and 58 / 202, 256 rows 85 / 253 and 59 / 230, 1024 rows 218 / 693 and 173 / 568; over 4099 x 256,
 // where big tiles are few, 1024 rows 29 / 40 and 30 / 63.
 const Shape& forward_shape(int64_t rows, int64_t vocab, int64_t cols, bool bf16) {
-  const Shape* two = SHAPES + (bf16 ? 0 : 2);
-  double us[2];
-  for (int i = 0; i < 2; ++i) {
-    const Shape& f = two[i];
+  int best = 0;
+  double least = 0.0;
+  const int from = first_shape(bf16), end = end_shape(bf16, rows <= Thin::BN);
+  for (int i = from; i < end; ++i) {
+    const Shape& f = SHAPES[i];
     const int64_t tiles = ((vocab + f.bm - 1) / f.bm) * ((rows + f.bn - 1) / f.bn), bk = bf16 ? 64 : 32;
-    us[i] = finish_time(tiles, (double)((cols + bk - 1) / bk) + TILE, 0, 1.0, f.slots) * f.slice_us;
+    const double slices = (double)((cols + bk - 1) / bk) + TILE, us = finish_time(tiles, slices, 0, 1.0, CUS) * f.share + slices * f.lag;
+    if (i == from || us < least) {
+      best = i;
+      least = us;
+    }
   }
-  return two[us[1] < us[0] ? 1 : 0];
+  return SHAPES[best];
 }
 
 // The cut depends on the sizes alone and takes some microseconds of the host to find: a thread keeps the last one.
@@ -840,9 +867,13 @@ Cut cut_of(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool want_dx) {
   };
   static thread_local Last last{-1, 0, 0, false, false, Cut{nullptr, 0, 1, false, 0.0}};
   if (last.rows != rows || last.vocab != vocab || last.cols != cols || last.bf16 != bf16 || last.want_dx != want_dx) {
-    const Shape* two = SHAPES + (bf16 ? 0 : 2);
-    const Cut a = cut_with(rows, vocab, cols, bf16, two[0], want_dx), b = cut_with(rows, vocab, cols, bf16, two[1], want_dx);
-    last = Last{rows, vocab, cols, bf16, want_dx, b.us < a.us ? b : a};
+    const int from = first_shape(bf16), end = end_shape(bf16, false);
+    Cut best = cut_with(rows, vocab, cols, bf16, SHAPES[from], want_dx);
+    for (int i = from + 1; i < end; ++i) {
+      const Cut c = cut_with(rows, vocab, cols, bf16, SHAPES[i], want_dx);
+      if (c.us < best.us) best = c;
+    }
+    last = Last{rows, vocab, cols, bf16, want_dx, best};
   }
   return last.cut;
 }
@@ -939,7 +970,8 @@ void launch_head_loss(const HeadDev& h, hipStream_t s) {
   switch (h.lay.kind) {
     case 0: logits<Big>(h, s); break;
     case 1: logits<Small>(h, s); break;
-    case 2: logits<Big32>(h, s); break;
+    case 2: logits<Thin>(h, s); break;
+    case 3: logits<Big32>(h, s); break;
     default: logits<Small32>(h, s); break;
   }
   const int tiles = h.lay.tiles, rl = h.rows <= 2048 ? 8 : 64, groups = (int)((h.rows + rl - 1) / rl);
@@ -961,7 +993,7 @@ void launch_head_backward(const HeadDev& h, hipStream_t s) {
   switch (h.lay.kind) {
     case 0: gradients<Big>(h, width, splits, s); break;
     case 1: gradients<Small>(h, width, splits, s); break;
-    case 2: gradients<Big32>(h, width, splits, s); break;
+    case 3: gradients<Big32>(h, width, splits, s); break;
     default: gradients<Small32>(h, width, splits, s); break;
   }
   if (h.dx.p) {

@@ -167,7 +167,12 @@ struct Src {
   int u, k;             // extent of the free index and of the contraction, in elements
 };
 
-template <class T, int BU, int NTHR, bool KC>
+// Which row of a wavefront's tiles a fragment's row is.  As they come, fragment i, row r: 16 i + r; an accumulator then holds four
+// neighbouring rows, 16 apart from those of the next tile.  PAIRS (the vocabulary rows of the logits): two tiles take 32 rows in turns of
+// four, so that the accumulators of the two hold eight neighbouring rows, 16 bytes of bf16.
+__device__ __forceinline__ constexpr int pair_row(int i, int r) { return 32 * (i >> 1) + 8 * (r >> 2) + 4 * (i & 1) + (r & 3); }
+
+template <class T, int BU, int NTHR, bool KC, bool PAIRS = false>
 struct Operand {
   static constexpr int ES = sizeof(T);
   static constexpr int BK = 128 / ES;                 // elements of the contraction in a slice
@@ -175,7 +180,8 @@ struct Operand {
   static constexpr int NL = BYTES / (16 * NTHR);      // 16-byte pieces of a thread
   static constexpr int RPC = BU * ES / 16;            // pieces of a row where k goes across
   static_assert(NL * 16 * NTHR == BYTES, "whole pieces");
-  // Where a piece stands.  KC: its place among the eight of its row is exchanged by the row's number.  Else pieces of 32 bytes (bf16; a
+  // Where a piece stands.  KC: its place among the eight of its row is exchanged by the row's number (PAIRS: by those of its bits in which the
+  // rows of one fragment differ).  Else pieces of 32 bytes (bf16; a
   // read touches rows 0 .. 3 and 8 .. 11 of a step at a time) or 64 bytes (fp32; rows 0, 4, 8 and 12) are exchanged by the row, over the
   // 256 bytes of all banks: where an LDS row is 128 or 64 bytes, its number's lowest bits say which half or quarter it lies in already.
   static_assert(KC || (ES == 2 && BU * ES == 64) || BU * ES == 128 || BU * ES >= 256, "exchanged inside a row");
@@ -184,6 +190,8 @@ struct Operand {
     if (BU * ES == 64) return (k >> 3) & 1;
     return BU * ES == 128 ? ((k >> 1) & 1) | ((k >> 2) & 2) : (k & 3) | ((k >> 1) & 4);
   }
+
+  static __device__ __forceinline__ int swz_kc(int row) { return PAIRS ? ((row >> 3) & 3) | ((row << 1) & 4) : row & 7; }
 
   int off[NL];          // byte offset of a thread's pieces in the slice that starts at k = 0, OOB outside the free index
   int k_in;             // KC: place of its pieces in the slice (the same for all)
@@ -194,7 +202,7 @@ struct Operand {
     k_in = 0;
     if (KC) {
       base = s.p + (int64_t)u0 * s.pitch;
-      k_in = ((tid & 7) ^ ((tid >> 3) & 7)) * (16 / ES);
+      k_in = ((tid & 7) ^ swz_kc(tid >> 3)) * (16 / ES);
 #pragma unroll
       for (int i = 0; i < NL; ++i) off[i] = ((tid + NTHR * i) >> 3) * (int)s.pitch + k_in * ES;
     } else {
@@ -228,20 +236,23 @@ struct Operand {
 // Fragment of 16 rows u .. u + 15 for step ks of a slice: eight (bf16) or four (fp32) values of the contraction for this lane.  `place` is
 // the lane's byte for ks = 0 and u = u0, the first row of the wavefront, the fragment's rows are u0 + 16 i: u0 / 16 is a multiple of the number of fragments, a
 // power of two, so that i can be exchanged with the lane's number by the same exclusive or.
-template <class T, int BU, bool KC>
+template <class T, int BU, bool KC, bool PAIRS = false>
 __device__ __forceinline__ int fragment_place(int u0) {
   constexpr int ES = sizeof(T);
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
-  if (KC) return (u0 + l16) * 128 + ((q ^ (l16 & 7)) << 4);
+  if (KC) {
+    const int row = PAIRS ? pair_row(0, l16) : l16;
+    return (u0 + row) * 128 + ((q ^ Operand<T, BU, 64, KC, PAIRS>::swz_kc(row)) << 4);
+  }
   // bf16: lane s of a block of 16 points at row s / 4, columns 4 (s % 4) .. + 3 of a 4 x 16 tile; lane i receives column i of the four rows
   const int k = ES == 2 ? q * 8 + (l16 >> 2) : q * 4;
   const int block = (u0 >> 4) ^ Operand<T, BU, 64, KC>::swz(k);
   return k * (BU * ES) + (ES == 2 ? (block << 5) + ((l16 & 3) << 3) : (block << 6) + (l16 << 2));
 }
-template <class T, int BU, bool KC>
+template <class T, int BU, bool KC, bool PAIRS = false>
 __device__ __forceinline__ u32x4 fragment(const lds_u8* lds, int place, int i, int ks) {
   constexpr int ES = sizeof(T);
-  if (KC) return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(lds + (place ^ (ks << 6)) + i * 2048);
+  if (KC) return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(lds + (place ^ (ks << 6)) + (PAIRS ? pair_row(i, 0) : 16 * i) * 128);
   lds += ks * (64 / ES) * (BU * ES);
   union {
     s16x4 h[2];
@@ -302,7 +313,7 @@ struct Acc {
 template <class C, bool AKC, bool BKC>
 struct Product {
   typedef typename C::T T;
-  typedef Operand<T, C::BM, C::THREADS, AKC> OA;
+  typedef Operand<T, C::BM, C::THREADS, AKC, AKC> OA;      // k along the rows: the logits' vocabulary rows
   typedef Operand<T, C::BN, C::THREADS, BKC> OB;
   static constexpr int BK = OA::BK, HALF = C::MT / 2;
   static constexpr int COPIES = OA::NL + OB::NL, LEFT = (C::DEPTH - 2) * COPIES;        // LEFT: copies still on their way at that point
@@ -326,7 +337,7 @@ struct Product {
     int place = pa;
     asm volatile("" : "+v"(place));      // worked out here every time: kept for all fragments the addresses would take too many registers
 #pragma unroll
-    for (int i = 0; i < HALF; ++i) f[i] = fragment<T, C::BM, AKC>(slice, place, half * HALF + i, ks);
+    for (int i = 0; i < HALF; ++i) f[i] = fragment<T, C::BM, AKC, AKC>(slice, place, half * HALF + i, ks);
   }
   __device__ __forceinline__ void read_b(u32x4 (&f)[C::NT], const lds_u8* slice, int ks) const {
     int place = pb;
@@ -410,7 +421,7 @@ __device__ __forceinline__ void product(const Src& A, const Src& B, int m0, int 
     for (int j = 0; j < C::NT; ++j) acc.v[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (k0 >= k1) return;
   Product<C, AKC, BKC> p{A, B, uniform(m0), uniform(n0), uniform(k1 < A.k ? (k1 < B.k ? k1 : B.k) : (A.k < B.k ? A.k : B.k)),
-                         fragment_place<typename C::T, C::BM, AKC>((wave % C::WM) * 16 * C::MT),
+                         fragment_place<typename C::T, C::BM, AKC, AKC>((wave % C::WM) * 16 * C::MT),
                          fragment_place<typename C::T, C::BN, BKC>((wave / C::WM) * 16 * C::NT)};
   p.run(uniform(k0), lds, acc);
 }
@@ -458,14 +469,14 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_
   const int* target = reinterpret_cast<const int*>(h.ws + h.lay.target);
   float2* part = reinterpret_cast<float2*>(h.ws + h.lay.part) + (int64_t)(tm * C::WM + wave % C::WM) * h.rows;
   float* hit = reinterpret_cast<float*>(h.ws + h.lay.hit);
-  const int v0 = m0 + um + 4 * q;
+  const int v0 = m0 + um + 8 * q;       // element (i, j, e): vocabulary row v0 + pair_row(i, e)
   // columns behind the vocabulary's end, in its last tile
   if (m0 + C::BM > h.vocab) {
 #pragma unroll
     for (int i = 0; i < C::MT; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (v0 + 16 * i + e >= h.vocab) {
+        if (v0 + pair_row(i, e) >= h.vocab) {
 #pragma unroll
           for (int j = 0; j < C::NT; ++j) acc.v[i][j][e] = -INFINITY;
         }
@@ -494,12 +505,12 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_
     if (row < n) {
       if (q == 0) part[row] = make_float2(top, sum);
       const int rel = target[row] - v0;
-      if (rel >= 0 && rel < 16 * C::MT && (rel & 15) < 4) {
+      if (rel >= 0 && rel < 16 * C::MT && (rel & 31) < 8) {
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < C::MT; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s = rel == 16 * i + e ? acc.v[i][j][e] : s;
+          for (int e = 0; e < 4; ++e) s = rel == pair_row(i, e) ? acc.v[i][j][e] : s;
         hit[row] = s;
       }
     }
@@ -508,7 +519,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_
 
 // Joins the tiles' maxima and sums: RL rows a workgroup, whose 1024 / RL slices share the tiles; each row's loss, and the workgroup's
 // sum of them.  RL = 8, 128 slices (one row over 32000 columns: 28.5 us with 16 of them, a chain of 63 loads) up to 2048 rows, which fill
-// the chip with such workgroups; beyond, RL = 64 and 16 slices, whose loads are whole lines.
+// the chip with such workgroups; beyond, RL = 16, whose loads are whole lines (8192 rows over 32000 columns 11 us with RL = 64, 6.8 with 16).
 template <int RL>
 __global__ __launch_bounds__(1024) void finish_kernel(HeadDev h, int tiles, int last) {
   constexpr int SL = 1024 / RL;
@@ -599,7 +610,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void piece_k
   for (int j = 0; j < C::NT; ++j) {
     const int row = n0 + un + 16 * j + l16;
     if (row >= n) continue;
-    const int target = reinterpret_cast<const int*>(h.ws + h.lay.target)[row] - (int)first - (m0 + um + 4 * q);
+    const int target = reinterpret_cast<const int*>(h.ws + h.lay.target)[row] - (int)first - (m0 + um + 8 * q);
     const float weight = reinterpret_cast<const float*>(h.ws + h.lay.weight)[row];
     const float lse = reinterpret_cast<const float*>(h.ws + h.lay.lse)[row], lse2 = lse * LOG2E;
     f32x4 p[C::MT];
@@ -613,7 +624,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void piece_k
 #pragma unroll
       for (int i = 0; i < C::MT; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[i][e] -= target == 16 * i + e ? 1.f : 0.f;
+        for (int e = 0; e < 4; ++e) p[i][e] -= target == pair_row(i, e) ? 1.f : 0.f;
     }
     if (h.row_weight) {
 #pragma unroll
@@ -623,20 +634,21 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void piece_k
 #pragma unroll
       for (int i = 0; i < C::MT; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[i][e] = m0 + um + 16 * i + 4 * q + e < width ? p[i][e] : 0.f;
+        for (int e = 0; e < 4; ++e) p[i][e] = m0 + um + 8 * q + pair_row(i, e) < width ? p[i][e] : 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < C::MT; ++i) {
-      const int v = m0 + um + 16 * i + 4 * q;
+    for (int i = 0; i < C::MT; i += 2) {
+      const int v = m0 + um + 8 * q + pair_row(i, 0);         // eight neighbouring columns of P
       T* to = P + (int64_t)row * pitch + v;
       if (v < pitch) {
         if (sizeof(T) == 2) {
-          u32x2 w;
-          w[0] = pack_bf16x2(p[i][0], p[i][1]);
-          w[1] = pack_bf16x2(p[i][2], p[i][3]);
-          *reinterpret_cast<u32x2*>(to) = w;
+          u32x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(p[i + e / 2][2 * (e & 1)], p[i + e / 2][2 * (e & 1) + 1]);
+          *reinterpret_cast<u32x4*>(to) = w;
         } else {
           *reinterpret_cast<f32x4*>(to) = p[i];
+          *reinterpret_cast<f32x4*>(to + 4) = p[i + 1];
         }
       }
     }
@@ -974,9 +986,9 @@ void launch_head_loss(const HeadDev& h, hipStream_t s) {
     case 3: logits<Big32>(h, s); break;
     default: logits<Small32>(h, s); break;
   }
-  const int tiles = h.lay.tiles, rl = h.rows <= 2048 ? 8 : 64, groups = (int)((h.rows + rl - 1) / rl);
+  const int tiles = h.lay.tiles, rl = h.rows <= 2048 ? 8 : 16, groups = (int)((h.rows + rl - 1) / rl);
   if (rl == 8) hipLaunchKernelGGL((finish_kernel<8>), dim3((unsigned)groups), dim3(1024), 0, s, h, tiles, groups == 1 ? 1 : 0);
-  else hipLaunchKernelGGL((finish_kernel<64>), dim3((unsigned)groups), dim3(1024), 0, s, h, tiles, 0);
+  else hipLaunchKernelGGL((finish_kernel<16>), dim3((unsigned)groups), dim3(1024), 0, s, h, tiles, 0);
   if (groups > 1) hipLaunchKernelGGL(total_kernel, dim3(1), dim3(256), 0, s, h, groups);
 }
 

@@ -14,6 +14,12 @@ import torch
 
 from . import binding as B
 
+try:        # the address alone: torch.cuda.current_stream makes an object for 2 us, as much as a small launch
+    from torch._C import _cuda_getCurrentRawStream as _raw_stream
+except ImportError:
+    def _raw_stream(device):
+        return torch.cuda.current_stream(device).cuda_stream
+
 _DT = {torch.float32: B.ADAPM_F32, torch.bfloat16: B.ADAPM_BF16, torch.float8_e4m3fn: B.ADAPM_E4M3}
 _REDUCTION = {"sum": B.ADAPM_REDUCE_SUM, "mean": B.ADAPM_REDUCE_MEAN}
 
@@ -65,6 +71,13 @@ def _rows(name, t, like, dtype, shape):
 def _new(t):
     """An output of the call's own making, whose elements are adjacent."""
     return B.adapm_rows_t(t.data_ptr(), t.shape[-1])
+
+
+def _empty(like, dtype=None):
+    """A tensor of like's shape whose elements are adjacent."""
+    if like.is_contiguous():
+        return torch.empty_like(like, dtype=dtype)
+    return like.new_empty(like.shape, dtype=dtype)
 
 
 def _stride(name, t):
@@ -123,11 +136,12 @@ def _dropout(p, rng, like):
 
 def _call(f, t, *args):
     """One library call on t's device and the current stream of that device."""
-    if t.get_device() == torch.cuda.current_device():
-        f(*args, torch.cuda.current_stream(t.device).cuda_stream)
+    at = t.get_device()
+    if at == torch.cuda.current_device():
+        f(*args, _raw_stream(at))
     else:
-        with torch.cuda.device(t.device):
-            f(*args, torch.cuda.current_stream(t.device).cuda_stream)
+        with torch.cuda.device(at):
+            f(*args, _raw_stream(at))
 
 
 _NO_ROWS = B.rows()
@@ -135,7 +149,7 @@ _NO_ROWS = B.rows()
 
 def _scratch(nbytes, like):
     # from the current stream's pool: PyTorch hands it to no other stream before the work queued here is done
-    return torch.empty(max(nbytes, 1), dtype=torch.uint8, device=like.device)
+    return like.new_empty(max(nbytes, 1), dtype=torch.uint8)
 
 
 def dropout(x: torch.Tensor, p: float, rng: Rng, residual: Optional[torch.Tensor] = None,
@@ -146,7 +160,7 @@ def dropout(x: torch.Tensor, p: float, rng: Rng, residual: Optional[torch.Tensor
     res = _NO_ROWS if residual is None else _rows("residual", residual, x, x.dtype, x.shape)
     drop = _dropout(p, rng, x) or B.adapm_dropout_t(0, 0, None, 0.0, 0)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _empty(x)
         y = _new(out)
     else:
         y = _rows("out", out, x, x.dtype, x.shape)
@@ -166,12 +180,12 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual:
         raise TypeError(f"out_dtype {out_dtype}: {x.dtype} or torch.float8_e4m3fn is wanted")
     drop = _dropout(p, rng, x)
     res = _NO_ROWS if residual is None else _rows("residual", residual, x, x.dtype, x.shape)
-    y = torch.empty(x.shape, dtype=out_dtype, device=x.device)
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    y = _empty(x, out_dtype)
+    rstd = x.new_empty(x.shape[:-1], dtype=torch.float32)
     scale = torch.empty_like(rstd) if out_dtype == torch.float8_e4m3fn else None
     h, hr = x, _NO_ROWS
     if residual is not None or drop is not None:
-        h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        h = _empty(x)
         hr = _new(h)
     _call(B.adapm_norm_forward, x, B.adapm_norm_t(n, cols, dt, wt, _DT[out_dtype], wt, eps, 0), xr, res, hr, w, _new(y),
           0 if scale is None else scale.data_ptr(), rstd.data_ptr(), drop)
@@ -192,12 +206,12 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, r
     up = _NO_ROWS if dh is None else _rows("dh", dh, dy, dy.dtype, dy.shape)
     hr = _rows("h", h, dy, dy.dtype, dy.shape)
     if dweight is None:
-        dweight = torch.empty(weight.shape, dtype=grad_dtype or weight.dtype, device=dy.device)
+        dweight = _empty(weight, grad_dtype)
     elif grad_dtype is not None and dweight.dtype != grad_dtype:
         raise TypeError(f"dweight: {dweight.dtype}, grad_dtype is {grad_dtype}")
     g = _vector("dweight", dweight, cols, dy, dweight.dtype)
     desc = B.adapm_norm_t(n, cols, dt, wt, dt, _float_type("dweight", dweight), 0.0, 0)
-    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
+    dx = _empty(dy)
     dres = dx if drop is None else torch.empty_like(dx)
     ws = _scratch(B.adapm_norm_workspace_bytes(desc), dy)
     _call(B.adapm_norm_backward, dy, desc, dyr, up, hr, w, r, _new(dx), _NO_ROWS if drop is None else _new(dres), g, drop, ws.data_ptr())
@@ -224,8 +238,8 @@ def head_loss(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, row_
     """Softmax cross entropy of x @ weight.T against targets (int64, one a row); rows whose target is outside the vocabulary (-100, say)
     do not count.  loss = scale * sum(row_weight * row_loss), divided by the number of rows that count where reduction is "mean"."""
     h, xr, w, t, rw = _head(x, weight, targets, row_weight, reduction, scale)
-    loss = torch.empty((), dtype=torch.float32, device=x.device)
-    row_loss = torch.empty(targets.shape, dtype=torch.float32, device=x.device)
+    loss = x.new_empty((), dtype=torch.float32)
+    row_loss = _empty(targets, torch.float32)
     lse = torch.empty_like(row_loss)
     size = B.adapm_head_workspace_bytes(h, w, False)
     ws = _scratch(size, x)
@@ -245,9 +259,9 @@ def head_backward(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, 
     if not need_dx and not need_dweight:
         raise ValueError("need_dx and need_dweight are both false")
     if need_dx and dx is None:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dx = _empty(x)
     if need_dweight and dweight is None:
-        dweight = torch.empty(weight.shape, dtype=x.dtype, device=x.device)
+        dweight = _empty(weight)
     gx = _rows("dx", dx, x, x.dtype, x.shape) if need_dx else _NO_ROWS
     gw = _rows("dweight", dweight, x, x.dtype, weight.shape) if need_dweight else _NO_ROWS
     size = B.adapm_head_workspace_bytes(h, w, True)

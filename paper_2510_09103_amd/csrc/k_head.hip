@@ -46,12 +46,19 @@ __device__ __forceinline__ float grad_factor(const HeadDev& h, int n) {
 }
 
 // ---- rows that count -------------------------------------------------------------------------------------------------
+// The few rows of a forward pass whose x can be read where it is are not packed (h.direct): each has a column of logits to itself, and
+// one that does not count is left out behind the products.
 constexpr int COUNT_ROWS = 1024;                      // rows of a workgroup of the count, and of an entry of its result
 constexpr int PACK_ROWS = 16;                         // rows of a workgroup of the packing
+constexpr int DIRECT_ROWS = 32;                       // most rows that are not packed: those that one workgroup joins
 
 __device__ __forceinline__ bool counts(const HeadDev& h, int64_t row) {
   const int64_t t = h.targets[row];
   return t >= 0 && t < h.vocab;
+}
+
+__device__ __forceinline__ int live_rows(const HeadDev& h) {
+  return h.direct ? (int)h.rows : reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
 }
 
 __global__ __launch_bounds__(256) void count_kernel(HeadDev h) {
@@ -444,6 +451,7 @@ __device__ __forceinline__ void place_tile(int id, int mt, int nt, int& m, int& 
 
 template <class T>
 __device__ __forceinline__ Src packed_x(const HeadDev& h, int n) {
+  if (h.direct) return Src{reinterpret_cast<const char*>(h.x.p), h.x.stride * (int)sizeof(T), n, h.cols};
   return Src{h.ws + h.lay.x, (int64_t)h.pitch * (int)sizeof(T), n, h.pitch};
 }
 template <class T>
@@ -457,7 +465,7 @@ template <class C>
 __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_kernel(HeadDev h, int mt) {
   typedef typename C::T T;
   HEAD_BUFFERS
-  const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
+  const int n = live_rows(h);
   const int nt = (n + C::BN - 1) / C::BN;
   if ((int)blockIdx.x >= mt * nt) return;
   int tm, tn;
@@ -504,7 +512,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_
     sum *= __builtin_amdgcn_exp2f(-rest);
     if (row < n) {
       if (q == 0) part[row] = make_float2(top, sum);
-      const int rel = target[row] - v0;
+      const int rel = (h.direct ? (counts(h, row) ? (int)h.targets[row] : -1) : target[row]) - v0;
       if (rel >= 0 && rel < 16 * C::MT && (rel & 31) < 8) {
         float s = 0.f;
 #pragma unroll
@@ -524,7 +532,7 @@ template <int RL>
 __global__ __launch_bounds__(1024) void finish_kernel(HeadDev h, int tiles, int last) {
   constexpr int SL = 1024 / RL;
   __shared__ float rm[SL][RL], rs[SL][RL];
-  const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
+  const int n = live_rows(h);
   const int l = threadIdx.x % RL, w = threadIdx.x / RL, row = blockIdx.x * RL + l;
   const float2* part = reinterpret_cast<const float2*>(h.ws + h.lay.part);
   double* sums = reinterpret_cast<double*>(h.ws + h.lay.sums);
@@ -552,18 +560,30 @@ __global__ __launch_bounds__(1024) void finish_kernel(HeadDev h, int tiles, int 
   }
   if (threadIdx.x >= 64) return;
   double part_loss = 0.0;
-  if (w == 0 && row < n) {
+  int counted = n;
+  bool in = w == 0 && row < n;
+  if (h.direct) {                                      // one workgroup
+    const bool live = in && counts(h, row);
+    if (in && !live) {
+      h.lse[row] = 0.f;
+      h.row_loss[row] = 0.f;
+    }
+    counted = __popcll(__ballot(live));
+    in = live;
+  }
+  if (in) {
     // the difference of the logits first, which is exact where they are near: a small loss keeps its digits
     const float log_sum = logf(s), lse = m + log_sum, loss = (m - reinterpret_cast<const float*>(h.ws + h.lay.hit)[row]) + log_sum;
-    const int to = reinterpret_cast<const int*>(h.ws + h.lay.list)[row];
+    const int to = h.direct ? row : reinterpret_cast<const int*>(h.ws + h.lay.list)[row];
     h.lse[to] = lse;
     h.row_loss[to] = loss;
-    part_loss = (double)reinterpret_cast<const float*>(h.ws + h.lay.weight)[row] * (double)loss;
+    const float weight = !h.direct ? reinterpret_cast<const float*>(h.ws + h.lay.weight)[row] : h.row_weight ? h.row_weight[row] : 1.f;
+    part_loss = (double)weight * (double)loss;
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) part_loss += __shfl_xor(part_loss, o);
   if (threadIdx.x) return;
-  if (last) *h.loss = (float)(part_loss * (double)h.scale / (h.mean ? (double)(n > 0 ? n : 1) : 1.0));
+  if (last) *h.loss = (float)(part_loss * (double)h.scale / (h.mean ? (double)(counted > 0 ? counted : 1) : 1.0));
   else sums[blockIdx.x] = part_loss;
 }
 
@@ -915,20 +935,24 @@ void gradients(const HeadDev& h, int64_t width, int splits, hipStream_t s) {
   }
 }
 
-void pack(const HeadDev& h, hipStream_t s) {
+void pack_x(const HeadDev& h, hipStream_t s) {
   if (h.rows > COUNT_ROWS)
     hipLaunchKernelGGL(count_kernel, dim3((unsigned)((h.rows + COUNT_ROWS - 1) / COUNT_ROWS)), dim3(256), 0, s, h);
   const dim3 grid((unsigned)((h.rows + PACK_ROWS - 1) / PACK_ROWS));
   if (h.bf16) hipLaunchKernelGGL((pack_kernel<uint16_t>), grid, dim3(256), 0, s, h);
   else hipLaunchKernelGGL((pack_kernel<float>), grid, dim3(256), 0, s, h);
+}
+void pack(const HeadDev& h, hipStream_t s) {
+  if (!h.direct) pack_x(h, s);
   if (h.w_packed) {
     const dim3 wgrid((unsigned)((h.vocab + PACK_ROWS - 1) / PACK_ROWS));
     if (h.bf16) hipLaunchKernelGGL((pack_w_kernel<uint16_t>), wgrid, dim3(256), 0, s, h);
     else hipLaunchKernelGGL((pack_w_kernel<float>), wgrid, dim3(256), 0, s, h);
   }
 }
-
 }  // namespace
+
+bool head_direct(int64_t rows) { return rows <= DIRECT_ROWS; }
 
 HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx) {
   const int64_t es = bf16 ? 2 : 4, pitch = up(cols, bf16 ? 64 : 32);
@@ -986,10 +1010,13 @@ void launch_head_loss(const HeadDev& h, hipStream_t s) {
     case 3: logits<Big32>(h, s); break;
     default: logits<Small32>(h, s); break;
   }
-  const int tiles = h.lay.tiles, rl = h.rows <= 2048 ? 8 : 16, groups = (int)((h.rows + rl - 1) / rl);
-  if (rl == 8) hipLaunchKernelGGL((finish_kernel<8>), dim3((unsigned)groups), dim3(1024), 0, s, h, tiles, groups == 1 ? 1 : 0);
-  else hipLaunchKernelGGL((finish_kernel<16>), dim3((unsigned)groups), dim3(1024), 0, s, h, tiles, 0);
-  if (groups > 1) hipLaunchKernelGGL(total_kernel, dim3(1), dim3(256), 0, s, h, groups);
+  const int tiles = h.lay.tiles, rl = h.rows <= 8 ? 8 : h.direct ? DIRECT_ROWS : h.rows <= 2048 ? 8 : 16, groups = (int)((h.rows + rl - 1) / rl);
+  const dim3 grid((unsigned)groups), block(1024);
+  const int last = groups == 1 ? 1 : 0;
+  if (rl == 8) hipLaunchKernelGGL((finish_kernel<8>), grid, block, 0, s, h, tiles, last);
+  else if (rl == 16) hipLaunchKernelGGL((finish_kernel<16>), grid, block, 0, s, h, tiles, last);
+  else hipLaunchKernelGGL((finish_kernel<DIRECT_ROWS>), grid, block, 0, s, h, tiles, last);
+  if (!last) hipLaunchKernelGGL(total_kernel, dim3(1), dim3(256), 0, s, h, groups);
 }
 
 void launch_head_backward(const HeadDev& h, hipStream_t s) {

@@ -78,8 +78,7 @@ adapm_status_t check_head(const adapm_head_t* h) {
   return ADAPM_OK;
 }
 
-// Rows of W that are whole 16-byte vectors are read where they are; others are copied into the workspace.  Its size is for the
-// worse case: the call alone sees the pointers.
+// Rows that are whole 16-byte vectors are read where they are; others are copied into the workspace.
 bool in_place(const adapm_head_t* h, const adapm_rows_t& w) {
   const int v = 16 / esize(h->dtype);
   return h->cols % v == 0 && w.stride % v == 0 && ((uintptr_t)w.data & 15) == 0;
@@ -113,6 +112,7 @@ adapm_status_t head_args(const adapm_head_t* h, adapm_rows_t x, adapm_rows_t wei
   d.loss = d.row_loss = d.lse = nullptr;
   d.ws = (char*)const_cast<void*>(workspace);
   d.w_packed = !in_place(h, weight);
+  d.direct = !backward && head_direct(h->rows) && in_place(h, x) && x.stride <= (1ll << 21);
   d.lay = head_layout(h->rows, h->vocab, h->cols, d.bf16, d.w_packed, backward, want_dx);
   if (h->rows && workspace_bytes < (size_t)d.lay.bytes)
     return fail(ADAPM_EINVAL, "workspace of %zu bytes, %lld are needed", workspace_bytes, (long long)d.lay.bytes);

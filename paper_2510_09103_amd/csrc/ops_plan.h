@@ -73,7 +73,11 @@ struct HeadDev {
   char* ws;
   HeadLayout lay;
   int w_packed;
+  int direct;                    // forward: x is read where it is
 };
+
+// whether a forward pass of so many rows reads x where it is, if x's rows are whole aligned vectors
+bool head_direct(int64_t rows);
 
 // backward: whether space for the gradients' pass is wanted (else the forward pass)
 HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx);

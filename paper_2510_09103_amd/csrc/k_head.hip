@@ -839,7 +839,7 @@ double finish_time(int64_t n1, double l1, int64_t n2, double l2, int64_t slots) 
 // which tiles come first are chosen by the time that follows from the tiles, for all rows and for two thirds of them: how many count is known on the device alone.  Loss and gradients of 8192 rows over
 // 32000 x 2048 / of 5500 over 32000 x 512, in four pieces of 134 MB 3527 / 1053 us (2 x 32 tiles of dW leave half of the chip idle in the
 // second), in three 3905 / 947, in two 3519 / 899, in one that the last-level cache does not hold 3606 / 872.
-Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, const Shape& f, bool want_dx) {
+Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, const Shape& f) {
   const int64_t es = bf16 ? 2 : 4, bk = 128 / es, slots = CUS * f.per_cu;
   const double us_per_byte = 1.0 / 4e6;
   int64_t fewest = (rows * vocab * es + PIECE_BYTES - 1) / PIECE_BYTES;
@@ -852,16 +852,16 @@ Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, const Shape& 
     const int64_t mp = (width + f.bm - 1) / f.bm, tw = mt * ((width + f.bn - 1) / f.bn), kv = width / bk;
     static const int parts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
     for (int sp : parts) {
-      if (sp > 1 && (!want_dx || sp * 256 > width)) break;
+      if (sp > 1 && sp * 256 > width) break;
       const double lx = (double)((kv + sp - 1) / sp) + TILE;
-      for (int dx_first = 0; dx_first < (want_dx ? 2 : 1); ++dx_first) {
+      for (int dx_first = 0; dx_first < 2; ++dx_first) {
         double t = 0.0;
         for (int64_t n = rows; n >= rows * 2 / 3 && n > 0; n = n == rows && rows > 2 ? rows * 2 / 3 : 0) {
-          const int64_t nt = (n + f.bn - 1) / f.bn, tx = want_dx ? mt * nt * sp : 0;
+          const int64_t nt = (n + f.bn - 1) / f.bn, tx = mt * nt * sp;
           const double lw = (double)((n + bk - 1) / bk) + TILE;
           t += (finish_time(mp * nt, (double)kd + TILE, 0, 1.0, slots) +
                 (dx_first ? finish_time(tx, lx, tw, lw, slots) : finish_time(tw, lw, tx, lx, slots))) * f.share * f.per_cu +
-               (want_dx ? 8.0 * (double)n * (double)cols * sp * us_per_byte : 0.0);
+               8.0 * (double)n * (double)cols * sp * us_per_byte;
         }
         t *= (double)pieces;
         if (best.width == 0 || t < best.us) best = Cut{&f, width, sp, dx_first != 0, t};
@@ -890,22 +890,23 @@ const Shape& forward_shape(int64_t rows, int64_t vocab, int64_t cols, bool bf16)
   return SHAPES[best];
 }
 
-// The cut depends on the sizes alone and takes some microseconds of the host to find: a thread keeps the last one.
-Cut cut_of(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool want_dx) {
+// The cut depends on the sizes alone (not on which gradients are wanted: the workspace is asked for without knowing) and takes some
+// microseconds of the host to find: a thread keeps the last one.
+Cut cut_of(int64_t rows, int64_t vocab, int64_t cols, bool bf16) {
   struct Last {
     int64_t rows, vocab, cols;
-    bool bf16, want_dx;
+    bool bf16;
     Cut cut;
   };
-  static thread_local Last last{-1, 0, 0, false, false, Cut{nullptr, 0, 1, false, 0.0}};
-  if (last.rows != rows || last.vocab != vocab || last.cols != cols || last.bf16 != bf16 || last.want_dx != want_dx) {
+  static thread_local Last last{-1, 0, 0, false, Cut{nullptr, 0, 1, false, 0.0}};
+  if (last.rows != rows || last.vocab != vocab || last.cols != cols || last.bf16 != bf16) {
     const int from = first_shape(bf16), end = end_shape(bf16, false);
-    Cut best = cut_with(rows, vocab, cols, bf16, SHAPES[from], want_dx);
+    Cut best = cut_with(rows, vocab, cols, bf16, SHAPES[from]);
     for (int i = from + 1; i < end; ++i) {
-      const Cut c = cut_with(rows, vocab, cols, bf16, SHAPES[i], want_dx);
+      const Cut c = cut_with(rows, vocab, cols, bf16, SHAPES[i]);
       if (c.us < best.us) best = c;
     }
-    last = Last{rows, vocab, cols, bf16, want_dx, best};
+    last = Last{rows, vocab, cols, bf16, best};
   }
   return last.cut;
 }
@@ -985,7 +986,7 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, boo
     l.hit = take(4 * rows);
     l.sums = take(8 * ((rows + 7) / 8));
   } else {
-    const Cut c = cut_of(rows > 0 ? rows : 1, vocab, cols, bf16, want_dx);
+    const Cut c = cut_of(rows > 0 ? rows : 1, vocab, cols, bf16);
     l.kind = c.shape->kind;
     l.width = c.width;
     l.splits = c.splits;

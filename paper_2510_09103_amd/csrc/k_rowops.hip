@@ -183,8 +183,8 @@ template <class T, int TPR, int NV>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_forward_kernel(NormDev a) {
   __shared__ float red[2][4];
   const int t = threadIdx.x % TPR;
-  const int64_t row = (int64_t)blockIdx.x * (threads_of(TPR) / TPR) + threadIdx.x / TPR;
-  if (row >= a.rows) return;         // whole wavefronts where TPR = 64, never where a workgroup is one row
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (threads_of(TPR) / TPR) + threadIdx.x / TPR;
+  if (row >= a.rows) return;         // whole wavefronts where TPR = 64, whole workgroups where one is a row
   const uint64_t offset = a.drop.thr ? drop_offset(a.drop) : 0;
   V8 h[NV];
   float sq = 0.f;
@@ -408,7 +408,9 @@ template <class T>
 void norm_forward(const NormDev& n, hipStream_t s) {
   const Shape f = shape_of(n.cols);
   const int rpb = threads_of(f.tpr) / f.tpr;
-  const dim3 grid((unsigned)((n.rows + rpb - 1) / rpb)), block((unsigned)threads_of(f.tpr));
+  // a dimension of the grid holds less than 2^32 threads
+  const int64_t groups = (n.rows + rpb - 1) / rpb, wide = groups < (1 << 20) ? groups : 1 << 20;
+  const dim3 grid((unsigned)wide, (unsigned)((groups + wide - 1) / wide)), block((unsigned)threads_of(f.tpr));
   if (f.tpr == 64) hipLaunchKernelGGL((norm_forward_kernel<T, 64, 1>), grid, block, 0, s, n);
   else if (f.tpr == 128) hipLaunchKernelGGL((norm_forward_kernel<T, 128, 1>), grid, block, 0, s, n);
   else if (f.nv == 1) hipLaunchKernelGGL((norm_forward_kernel<T, 256, 1>), grid, block, 0, s, n);

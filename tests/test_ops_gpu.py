@@ -270,6 +270,15 @@ def test_head_in_several_pieces(rows, vocab, cols, dtype):
     check_head(*problem(rows, vocab, cols, dtype, 0.1))
 
 
+def test_head_in_several_pieces_one_gradient_at_a_time():
+    """The scratch that is asked for without knowing which gradients are wanted serves either of them alone, with the same bits."""
+    x, W, t = problem(16000, 20000, 16, BF16, 0.1)
+    r = ops.head_loss(x, W, t)
+    dx, dW = ops.head_backward(x, W, t, r.lse)
+    assert torch.equal(ops.head_backward(x, W, t, r.lse, need_dweight=False)[0], dx)
+    assert torch.equal(ops.head_backward(x, W, t, r.lse, need_dx=False)[1], dW)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_head_large_logits(dtype):
     """Logits of some hundreds: the maximum is taken out before the exponential, a sure row has loss 0 and no gradient."""

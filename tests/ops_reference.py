@@ -21,8 +21,8 @@ def threshold(p):
     return min(65535, int(65536 * float(torch.tensor(p, dtype=torch.float32)) + 0.5))
 
 
-def factors(rows, cols, p, seed, offset):
-    """What dropout multiplies every element by, 0 or 65536 / (65536 - threshold), as float64 on the CPU."""
+def factors(rows, cols, p, seed, offset, first=0):
+    """What dropout multiplies every element by, 0 or 65536 / (65536 - threshold), as float64 on the CPU: rows first .. first + rows."""
     thr = threshold(p)
     out = torch.empty(rows, cols, dtype=torch.float64)
     key = (seed & LOW, seed >> 32 & LOW)
@@ -30,7 +30,7 @@ def factors(rows, cols, p, seed, offset):
     for r in range(rows):
         bits = []
         for g in range((cols + 7) // 8):
-            for w in philox((g, r & LOW, offset & LOW, offset >> 32), key):
+            for w in philox((g, (first + r) & LOW, offset & LOW, offset >> 32), key):
                 bits += [w & 0xFFFF, w >> 16]
         out[r] = torch.tensor([65536.0 / (65536 - thr) if b >= thr else 0.0 for b in bits[:cols]], dtype=torch.float64)
     return out

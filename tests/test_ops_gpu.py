@@ -310,6 +310,52 @@ def test_head_gradient_is_the_derivative():
             assert abs(slope - got.view(-1)[i].item()) < 1e-6
 
 
+# ---- places past 32 bits -----------------------------------------------------------------------------------------------
+
+def test_dropout_of_more_than_2_to_the_32_elements():
+    rows, cols = 66000, 65600
+    x = torch.ones(rows, cols, dtype=BF16, device="cuda")
+    assert x.numel() > 1 << 32
+    ops.dropout(x, 0.25, ops.Rng(8, 9), out=x)
+    for first in (0, 65535, rows - 1):
+        f = R.factors(1, cols, 0.25, 8, 9, first)[0].to(BF16)
+        assert torch.equal(x[first].cpu(), f)
+
+
+def test_norm_of_more_than_2_to_the_32_elements():
+    rows, cols = 262500, 16384
+    x = torch.empty(rows, cols, dtype=BF16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))
+    w = torch.ones(cols, dtype=BF16, device="cuda")
+    assert x.numel() > 1 << 32
+    n = ops.rms_norm(x, w)
+    for part in (slice(0, 3), slice(rows // 2, rows // 2 + 2), slice(rows - 3, rows)):
+        assert torch.equal(n.y[part], ops.rms_norm(x[part].clone(), w).y)
+    dx, _, dw = ops.rms_norm_backward(n.y, x, w, n.rstd, grad_dtype=F32)
+    assert torch.equal(dx[-3:], ops.rms_norm_backward(n.y[-3:].clone(), x[-3:].clone(), w, n.rstd[-3:].clone())[0])
+    # sum over the rows of y^2: rows times the mean square of a normed row, 1, within five standard deviations (2 / rows)^0.5
+    assert abs(dw.double().mean().item() / rows - 1) < 5 * (2 / rows / cols) ** 0.5 + 1e-4
+
+
+def test_head_of_more_than_2_to_the_32_bytes():
+    rows, vocab, cols = 3, 1060000, 2048
+    W = torch.empty(vocab, cols, dtype=BF16, device="cuda").normal_(std=0.05, generator=torch.Generator("cuda").manual_seed(2))
+    assert W.numel() * 2 > 1 << 32
+    x = randn(rows, cols, dtype=BF16, seed=3)
+    t = torch.tensor([0, vocab - 1, vocab // 2], device="cuda")
+    s = torch.cat([x.double() @ c.double().t() for c in W.split(100000)], 1)
+    off = (cols + 2) * R.U * (x.double().abs() @ W[:1000].double().abs().t()).amax() * 4        # rows of W are alike: four times the largest of 1000
+    r = ops.head_loss(x, W, t)
+    lse = torch.logsumexp(s, 1)
+    R.within("lse", r.lse, lse, off + 2.0 ** -19)
+    R.within("row_loss", r.row_loss, lse - s.gather(1, t[:, None])[:, 0], 2 * off + 2.0 ** -18)
+    _, dW = ops.head_backward(x, W, t, r.lse)
+    at = torch.tensor([0, 1, vocab // 2, vocab - 2, vocab - 1], device="cuda")
+    p = (s[:, at] - lse[:, None]).exp() - (t[:, None] == at[None]).double()
+    want = p.t() @ x.double() / rows
+    # P rounded to bf16, its exponentials off by twice a logit's bound; then dW rounded
+    R.within("dweight", dW[at], want, ((2.0 ** -8 + 4 * off + 2.0 ** -18) * p.abs()).t() @ x.double().abs() / rows * (1 + 2.0 ** -7), BF16)
+
+
 # ---- together ---------------------------------------------------------------------------------------------------------
 
 def model_end(x, res, g, W, t, rng):

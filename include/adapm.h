@@ -297,7 +297,7 @@ adapm_status_t adapm_head_loss(const adapm_head_t* h, adapm_rows_t x, adapm_rows
 /* Gradients of upstream * loss (upstream_dev: one float, NULL: 1) by x and W, for the same arguments and the lse of
  * adapm_head_loss.  Either of dx and dweight may have data = NULL; rows that do not count get dx = 0.  All vocab rows of dweight
  * are written: for the output head of a table that buffer is the block's gradient in adapm_step.  bf16: P = w (softmax - onehot) is
- * rounded to bf16 between the products. */
+ * rounded to bf16 between the products (up to 32 rows, with row weights up to 1024, it is kept as two bf16 numbers). */
 adapm_status_t adapm_head_backward(const adapm_head_t* h, adapm_rows_t x, adapm_rows_t weight, const int64_t* targets_dev,
                                    const float* row_weight_dev, const float* lse_dev, const float* upstream_dev,
                                    adapm_rows_t dx, adapm_rows_t dweight, void* workspace_dev, size_t workspace_bytes,

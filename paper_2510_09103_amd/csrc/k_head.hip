@@ -45,6 +45,15 @@ __device__ __forceinline__ float grad_factor(const HeadDev& h, int n) {
   return h.mean ? f / (float)(n > 0 ? n : 1) : f;
 }
 
+// Few rows: P travels as two bf16 numbers, P rounded and what that has left out, 2^-17 of it in all.  A gradient in bf16 has an error of
+// its own, 1.7e-3 of it in root mean square.  P rounded once brings that to 1.2 times as much: the targets' elements are most of it, and
+// those near -1 lose little.  With weights on the rows they lose as much as any number, and it is 1.42 times; what a single P has lost
+// averages over the rows that a gradient comes from, or does not where they are few (1.26 times at worst in 40 problems of 32 rows, with
+// weights 1.77; 1.51 of 700 rows, 1.46 of 1500).  The second numbers are more rows of P, against a second copy of x: dW's contraction
+// takes them in, and dx's sums for them are added to those of the first.  32 rows over 32000 x 2048 109 -> 115 us, 512 with weights
+// 229 -> 339.
+constexpr int64_t TWIN_ROWS = 32, TWIN_ROWS_WEIGHTED = 1024;
+
 // ---- rows that count -------------------------------------------------------------------------------------------------
 // The few rows of a forward pass whose x can be read where it is are not packed (h.direct): each has a column of logits to itself, and
 // one that does not count is left out behind the products.
@@ -103,16 +112,18 @@ __global__ __launch_bounds__(256) void pack_kernel(HeadDev h) {
   const int* counted = reinterpret_cast<const int*>(h.ws + h.lay.counts);
   for (int64_t i = threadIdx.x; i < b0; i += 256) c += counted[i];
   for (int64_t row = b0 * COUNT_ROWS + threadIdx.x; row < r0; row += 256) c += counts(h, row) ? 1 : 0;
+  if (h.twin)          // few rows: all that count, in the upper half
+    for (int64_t row = threadIdx.x; row < h.rows; row += 256) c += counts(h, row) ? 1 << 16 : 0;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) c += __shfl_xor(c, o);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
   __syncthreads();
+  const int sum = red[0] + red[1] + red[2] + red[3], before = h.twin ? sum & 0xffff : sum, all = sum >> 16;
   if (threadIdx.x < 64) {
     const int64_t row = r0 + threadIdx.x;
     const bool in = threadIdx.x < PACK_ROWS && row < h.rows;
     const bool live = in && counts(h, row);
     const unsigned long long m = __ballot(live);
-    const int before = red[0] + red[1] + red[2] + red[3];
     const int j = before + __popcll(m & ((1ull << threadIdx.x) - 1));
     if (in) {
       place[threadIdx.x] = live ? j : -1;
@@ -136,8 +147,10 @@ __global__ __launch_bounds__(256) void pack_kernel(HeadDev h) {
   for (int i = threadIdx.x; i < PACK_ROWS * per; i += 256) {
     const int r = i / per, c0 = (i - r * per) * V;
     if (r0 + r >= h.rows || place[r] < 0) continue;
-    *reinterpret_cast<u32x4*>(reinterpret_cast<T*>(h.ws + h.lay.x) + (int64_t)place[r] * h.pitch + c0) =
-        piece_of(reinterpret_cast<const T*>(h.x.p) + (r0 + r) * h.x.stride, c0, h.cols);
+    T* to = reinterpret_cast<T*>(h.ws + h.lay.x) + (int64_t)place[r] * h.pitch + c0;
+    const u32x4 v = piece_of(reinterpret_cast<const T*>(h.x.p) + (r0 + r) * h.x.stride, c0, h.cols);
+    *reinterpret_cast<u32x4*>(to) = v;
+    if (h.twin) *reinterpret_cast<u32x4*>(to + (int64_t)all * h.pitch) = v;
   }
 }
 
@@ -666,6 +679,12 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void piece_k
 #pragma unroll
           for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(p[i + e / 2][2 * (e & 1)], p[i + e / 2][2 * (e & 1) + 1]);
           *reinterpret_cast<u32x4*>(to) = w;
+          if (h.twin) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              w[e] = pack_bf16x2(p[i + e / 2][2 * (e & 1)] - bf16lo(w[e]), p[i + e / 2][2 * (e & 1) + 1] - bf16hi(w[e]));
+            *reinterpret_cast<u32x4*>(to + (int64_t)n * pitch) = w;
+          }
         } else {
           *reinterpret_cast<f32x4*>(to) = p[i];
           *reinterpret_cast<f32x4*>(to + 4) = p[i + 1];
@@ -691,7 +710,7 @@ template <class C>
 __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_kernel(HeadDev h, GradPlan g) {
   typedef typename C::T T;
   HEAD_BUFFERS
-  const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
+  const int live = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n, n = live << h.twin;      // rows of P and of packed x
   const char* P = h.ws + h.lay.p;
   const int64_t pp = g.pitch * (int64_t)sizeof(T);
   const int n_dw = g.mt * g.nt_w;
@@ -704,7 +723,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_ke
     const int m0 = tm * C::BM, n0 = tn * C::BN;
     product<C, false, false>(Src{h.ws + h.lay.x, (int64_t)h.pitch * (int)sizeof(T), h.pitch, n}, Src{P, pp, (int)g.pitch, n}, m0, n0, 0, n,
                              lds, acc);
-    const float f = grad_factor(h, n);
+    const float f = grad_factor(h, live);
 #pragma unroll
     for (int j = 0; j < C::NT; ++j) {
       const int v = n0 + un + 16 * j + l16;
@@ -744,7 +763,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_ke
   W.u = cols;
   W.k = g.width;
   product<C, false, true>(W, Src{P, pp, n, (int)g.pitch}, m0, n0, k0, k1, lds, acc);
-  float* sum = reinterpret_cast<float*>(h.ws + h.lay.acc) + (int64_t)split * h.rows * h.pitch;
+  float* sum = reinterpret_cast<float*>(h.ws + h.lay.acc) + (int64_t)split * (h.rows << h.twin) * h.pitch;
 #pragma unroll
   for (int j = 0; j < C::NT; ++j) {
     const int row = n0 + un + 16 * j + l16;
@@ -766,15 +785,32 @@ __global__ __launch_bounds__(256) void dx_kernel(HeadDev h, int splits) {
   const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
   const int64_t row = blockIdx.x;
   const int j = reinterpret_cast<const int*>(h.ws + h.lay.place)[row];
-  const float* sum = reinterpret_cast<const float*>(h.ws + h.lay.acc);
   const float f = grad_factor(h, n);
   T* to = reinterpret_cast<T*>(h.dx.p) + row * h.dx.stride;
-  for (int c = threadIdx.x; c < h.cols; c += 256) {
-    float x = 0.f;
-    if (j >= 0)
-      for (int s = 0; s < splits; ++s) x += sum[((int64_t)s * h.rows + j) * h.pitch + c];
+  const int64_t part = (h.rows << h.twin) * (int64_t)h.pitch;
+  const float* sum = reinterpret_cast<const float*>(h.ws + h.lay.acc) + (j < 0 ? 0 : (int64_t)j * h.pitch);
+  for (int c = threadIdx.x * 4; c < h.cols; c += 1024) {
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    if (j >= 0) {
+      for (int s = 0; s < splits; ++s) x += *reinterpret_cast<const f32x4*>(sum + s * part + c);
+      if (h.twin)
+        for (int s = 0; s < splits; ++s) x += *reinterpret_cast<const f32x4*>(sum + s * part + (int64_t)n * h.pitch + c);
+    }
     x *= f;
-    to[c] = sizeof(T) == 2 ? (T)pack_bf16x2(x, 0.f) : (T)x;
+    if (c + 4 <= h.cols) {
+      if (sizeof(T) == 2) {
+        u32x2 w;
+        w[0] = pack_bf16x2(x[0], x[1]);
+        w[1] = pack_bf16x2(x[2], x[3]);
+        *reinterpret_cast<u32x2_e2*>(to + c) = w;
+      } else {
+        *reinterpret_cast<f32x4_e4*>(to + c) = x;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c + e < h.cols) to[c + e] = sizeof(T) == 2 ? (T)pack_bf16x2(x[e], 0.f) : (T)x[e];
+    }
   }
 }
 
@@ -805,6 +841,10 @@ int first_shape(bool bf16) { return bf16 ? 0 : 3; }
 int end_shape(bool bf16, bool thin) { return !bf16 ? 5 : thin ? 3 : 2; }
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+}  // namespace
+int head_twin(int64_t rows, bool bf16, bool weighted) { return bf16 && rows <= (weighted ? TWIN_ROWS_WEIGHTED : TWIN_ROWS) ? 1 : 0; }
+namespace {
 
 // How the backward pass is cut.
 struct Cut {
@@ -839,10 +879,10 @@ double finish_time(int64_t n1, double l1, int64_t n2, double l2, int64_t slots) 
 // which tiles come first are chosen by the time that follows from the tiles, for all rows and for two thirds of them: how many count is known on the device alone.  Loss and gradients of 8192 rows over
 // 32000 x 2048 / of 5500 over 32000 x 512, in four pieces of 134 MB 3527 / 1053 us (2 x 32 tiles of dW leave half of the chip idle in the
 // second), in three 3905 / 947, in two 3519 / 899, in one that the last-level cache does not hold 3606 / 872.
-Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, const Shape& f) {
+Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, int twin, const Shape& f) {
   const int64_t es = bf16 ? 2 : 4, bk = 128 / es, slots = CUS * f.per_cu;
   const double us_per_byte = 1.0 / 4e6;
-  int64_t fewest = (rows * vocab * es + PIECE_BYTES - 1) / PIECE_BYTES;
+  int64_t fewest = ((rows << twin) * vocab * es + PIECE_BYTES - 1) / PIECE_BYTES;
   const int64_t most = (vocab + 2047) / 2048;                         // pieces of at least 2048
   if (fewest > most) fewest = most;
   const int64_t mt = (cols + f.bm - 1) / f.bm, kd = (cols + bk - 1) / bk;
@@ -857,11 +897,11 @@ Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, const Shape& 
       for (int dx_first = 0; dx_first < 2; ++dx_first) {
         double t = 0.0;
         for (int64_t n = rows; n >= rows * 2 / 3 && n > 0; n = n == rows && rows > 2 ? rows * 2 / 3 : 0) {
-          const int64_t nt = (n + f.bn - 1) / f.bn, tx = mt * nt * sp;
-          const double lw = (double)((n + bk - 1) / bk) + TILE;
+          const int64_t nt = (n + f.bn - 1) / f.bn, n2 = n << twin, tx = mt * ((n2 + f.bn - 1) / f.bn) * sp;
+          const double lw = (double)((n2 + bk - 1) / bk) + TILE;
           t += (finish_time(mp * nt, (double)kd + TILE, 0, 1.0, slots) +
                 (dx_first ? finish_time(tx, lx, tw, lw, slots) : finish_time(tw, lw, tx, lx, slots))) * f.share * f.per_cu +
-               8.0 * (double)n * (double)cols * sp * us_per_byte;
+               8.0 * (double)n2 * (double)cols * sp * us_per_byte;
         }
         t *= (double)pieces;
         if (best.width == 0 || t < best.us) best = Cut{&f, width, sp, dx_first != 0, t};
@@ -891,19 +931,20 @@ const Shape& forward_shape(int64_t rows, int64_t vocab, int64_t cols, bool bf16)
 }
 
 // The cut depends on the sizes alone (not on which gradients are wanted: the workspace is asked for without knowing) and takes some
-// microseconds of the host to find: a thread keeps the last one.
-Cut cut_of(int64_t rows, int64_t vocab, int64_t cols, bool bf16) {
+// microseconds of the host to find: a thread keeps the last ones.
+Cut cut_of(int64_t rows, int64_t vocab, int64_t cols, bool bf16, int twin) {
   struct Last {
     int64_t rows, vocab, cols;
     bool bf16;
     Cut cut;
   };
-  static thread_local Last last{-1, 0, 0, false, Cut{nullptr, 0, 1, false, 0.0}};
+  static thread_local Last kept[2] = {{-1, 0, 0, false, Cut{nullptr, 0, 1, false, 0.0}}, {-1, 0, 0, false, Cut{nullptr, 0, 1, false, 0.0}}};
+  Last& last = kept[twin];
   if (last.rows != rows || last.vocab != vocab || last.cols != cols || last.bf16 != bf16) {
     const int from = first_shape(bf16), end = end_shape(bf16, false);
-    Cut best = cut_with(rows, vocab, cols, bf16, SHAPES[from]);
+    Cut best = cut_with(rows, vocab, cols, bf16, twin, SHAPES[from]);
     for (int i = from + 1; i < end; ++i) {
-      const Cut c = cut_with(rows, vocab, cols, bf16, SHAPES[i]);
+      const Cut c = cut_with(rows, vocab, cols, bf16, twin, SHAPES[i]);
       if (c.us < best.us) best = c;
     }
     last = Last{rows, vocab, cols, bf16, best};
@@ -925,14 +966,15 @@ void gradients(const HeadDev& h, int64_t width, int splits, hipStream_t s) {
     g.width = (int)(h.vocab - first < width ? h.vocab - first : width);
     g.pitch = width;
     const int mp = (int)((up(g.width, 64) + C::BM - 1) / C::BM), np = (int)((h.rows + C::BN - 1) / C::BN);
+    const int nx = (int)(((h.rows << h.twin) + C::BN - 1) / C::BN);
     hipLaunchKernelGGL((piece_kernel<C>), dim3((unsigned)(mp * np)), dim3(C::THREADS), 0, s, h, first, g.width, width, mp);
     g.mt = (h.cols + C::BM - 1) / C::BM;
     g.splits = h.dx.p ? splits : 0;
     g.k_split = (int)up((g.width + splits - 1) / splits, 64);
     g.nt_w = h.dw.p ? (g.width + C::BN - 1) / C::BN : 0;
     g.begin = first == 0;
-    g.first_dw = h.lay.dx_first && h.dx.p ? g.mt * np * g.splits : 0;
-    hipLaunchKernelGGL((grad_kernel<C>), dim3((unsigned)(g.mt * (g.nt_w + np * g.splits))), dim3(C::THREADS), 0, s, h, g);
+    g.first_dw = h.lay.dx_first && h.dx.p ? g.mt * nx * g.splits : 0;
+    hipLaunchKernelGGL((grad_kernel<C>), dim3((unsigned)(g.mt * (g.nt_w + nx * g.splits))), dim3(C::THREADS), 0, s, h, g);
   }
 }
 
@@ -955,8 +997,8 @@ void pack(const HeadDev& h, hipStream_t s) {
 
 bool head_direct(int64_t rows) { return rows <= DIRECT_ROWS; }
 
-HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx) {
-  const int64_t es = bf16 ? 2 : 4, pitch = up(cols, bf16 ? 64 : 32);
+HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx, int twin) {
+  const int64_t es = bf16 ? 2 : 4, pitch = up(cols, bf16 ? 64 : 32), rows2 = rows << twin;
   HeadLayout l;
   l.width = 0;
   l.splits = 0;
@@ -975,7 +1017,7 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, boo
   l.target = take(4 * rows);
   l.weight = take(4 * rows);
   l.lse = take(4 * rows);
-  l.x = take(rows * pitch * es);
+  l.x = take(rows2 * pitch * es);
   l.w = w_packed ? take(vocab * pitch * es) : -1;
   l.part = l.hit = l.sums = l.p = l.acc = -1;
   if (!backward) {
@@ -986,13 +1028,13 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, boo
     l.hit = take(4 * rows);
     l.sums = take(8 * ((rows + 7) / 8));
   } else {
-    const Cut c = cut_of(rows > 0 ? rows : 1, vocab, cols, bf16);
+    const Cut c = cut_of(rows > 0 ? rows : 1, vocab, cols, bf16, twin);
     l.kind = c.shape->kind;
     l.width = c.width;
     l.splits = c.splits;
     l.dx_first = c.dx_first;
-    l.p = take(rows * c.width * es);
-    if (want_dx) l.acc = take(4 * rows * pitch * c.splits);
+    l.p = take(rows2 * c.width * es);
+    if (want_dx) l.acc = take(4 * rows2 * pitch * c.splits);
   }
   l.bytes = at;
   return l;

@@ -112,8 +112,9 @@ adapm_status_t head_args(const adapm_head_t* h, adapm_rows_t x, adapm_rows_t wei
   d.loss = d.row_loss = d.lse = nullptr;
   d.ws = (char*)const_cast<void*>(workspace);
   d.w_packed = !in_place(h, weight);
+  d.twin = backward ? head_twin(h->rows, d.bf16, row_weight != nullptr) : 0;
   d.direct = !backward && head_direct(h->rows) && in_place(h, x) && x.stride <= (1ll << 21);
-  d.lay = head_layout(h->rows, h->vocab, h->cols, d.bf16, d.w_packed, backward, want_dx);
+  d.lay = head_layout(h->rows, h->vocab, h->cols, d.bf16, d.w_packed, backward, want_dx, d.twin);
   if (h->rows && workspace_bytes < (size_t)d.lay.bytes)
     return fail(ADAPM_EINVAL, "workspace of %zu bytes, %lld are needed", workspace_bytes, (long long)d.lay.bytes);
   *out = d;
@@ -217,7 +218,14 @@ adapm_status_t adapm_norm_backward(const adapm_norm_t* n, adapm_rows_t dy, adapm
 
 size_t adapm_head_workspace_bytes(const adapm_head_t* h, adapm_rows_t weight, int32_t backward) {
   if (check_head(h) != ADAPM_OK) return 0;
-  return (size_t)head_layout(h->rows, h->vocab, h->cols, h->dtype == ADAPM_BF16, !in_place(h, weight), backward != 0, true).bytes;
+  // for a call with or without weights on its rows
+  const bool bf16 = h->dtype == ADAPM_BF16, packed = !in_place(h, weight);
+  int64_t bytes = 0;
+  for (int weighted = 0; weighted < (backward ? 2 : 1); ++weighted) {
+    const int64_t b = head_layout(h->rows, h->vocab, h->cols, bf16, packed, backward != 0, true, backward ? head_twin(h->rows, bf16, weighted != 0) : 0).bytes;
+    bytes = b > bytes ? b : bytes;
+  }
+  return (size_t)bytes;
 }
 
 adapm_status_t adapm_head_loss(const adapm_head_t* h, adapm_rows_t x, adapm_rows_t weight, const int64_t* targets,

@@ -74,13 +74,17 @@ struct HeadDev {
   HeadLayout lay;
   int w_packed;
   int direct;                    // forward: x is read where it is
+  int twin;                      // backward: P as two numbers
 };
+
+// backward: 1 if P of so many rows is kept as two numbers
+int head_twin(int64_t rows, bool bf16, bool weighted);
 
 // whether a forward pass of so many rows reads x where it is, if x's rows are whole aligned vectors
 bool head_direct(int64_t rows);
 
 // backward: whether space for the gradients' pass is wanted (else the forward pass)
-HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx);
+HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx, int twin);
 void launch_head_loss(const HeadDev& h, hipStream_t s);
 void launch_head_backward(const HeadDev& h, hipStream_t s);
 

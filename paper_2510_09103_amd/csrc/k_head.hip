@@ -551,12 +551,17 @@ __global__ __launch_bounds__(1024) void finish_kernel(HeadDev h, int tiles, int 
   double* sums = reinterpret_cast<double*>(h.ws + h.lay.sums);
   float m = -INFINITY, s = 0.f;
   if (row < n)
-    for (int t = w; t < tiles; t += SL) {
-      const float2 p = part[(int64_t)t * h.rows + row];
-      if (p.y == 0.f) continue;                        // a tile behind the vocabulary's end
-      const float top = fmaxf(m, p.x);
-      s = (s == 0.f ? 0.f : s * __builtin_amdgcn_exp2f((m - top) * LOG2E)) + p.y * __builtin_amdgcn_exp2f((p.x - top) * LOG2E);
-      m = top;
+    for (int t0 = w; t0 < tiles; t0 += 4 * SL) {
+      float2 p[4];                                     // requested together
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = t0 + i * SL < tiles ? part[(int64_t)(t0 + i * SL) * h.rows + row] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (p[i].y == 0.f) continue;                   // a tile behind the vocabulary's end
+        const float top = fmaxf(m, p[i].x);
+        s = (s == 0.f ? 0.f : s * __builtin_amdgcn_exp2f((m - top) * LOG2E)) + p[i].y * __builtin_amdgcn_exp2f((p[i].x - top) * LOG2E);
+        m = top;
+      }
     }
   rm[w][l] = m;
   rs[w][l] = s;

@@ -201,7 +201,8 @@ struct Operand {
   static constexpr int RPC = BU * ES / 16;            // pieces of a row where k goes across
   static_assert(NL * 16 * NTHR == BYTES, "whole pieces");
   // Where a piece stands.  KC: its place among the eight of its row is exchanged by the row's number (PAIRS: by those of its bits in which the
-  // rows of one fragment differ).  Else pieces of 32 bytes (bf16; a
+  // rows of one fragment differ).  The 256 bytes of a cycle are those of lanes 0 - 3, 12 - 15, 20 - 23, 24 - 27, and so on in fours:
+  // rows 1 and 2 of four go with the next piece of rows 0 and 3.  Else pieces of 32 bytes (bf16; a
   // read touches rows 0 .. 3 and 8 .. 11 of a step at a time) or 64 bytes (fp32; rows 0, 4, 8 and 12) are exchanged by the row, over the
   // 256 bytes of all banks: where an LDS row is 128 or 64 bytes, its number's lowest bits say which half or quarter it lies in already.
   static_assert(KC || (ES == 2 && BU * ES == 64) || BU * ES == 128 || BU * ES >= 256, "exchanged inside a row");
@@ -211,7 +212,11 @@ struct Operand {
     return BU * ES == 128 ? ((k >> 1) & 1) | ((k >> 2) & 2) : (k & 3) | ((k >> 1) & 4);
   }
 
-  static __device__ __forceinline__ int swz_kc(int row) { return PAIRS ? ((row >> 3) & 3) | ((row << 1) & 4) : row & 7; }
+  static __device__ __forceinline__ int swz_kc(int row) {
+    if (!PAIRS) return row & 7;
+    const int a = row >> 3;
+    return ((a ^ (a << 1 & 2)) & 3) | (row << 1 & 4);
+  }
 
   int off[NL];          // byte offset of a thread's pieces in the slice that starts at k = 0, OOB outside the free index
   int k_in;             // KC: place of its pieces in the slice (the same for all)

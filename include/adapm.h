@@ -276,7 +276,8 @@ adapm_status_t adapm_norm_backward(const adapm_norm_t* n, adapm_rows_t dy, adapm
  * kept.  f = scale, divided by the number of rows that count with ADAPM_REDUCE_MEAN. */
 typedef enum { ADAPM_REDUCE_SUM = 0, ADAPM_REDUCE_MEAN = 1 } adapm_reduction_t;
 typedef struct {
-  int64_t rows, vocab, cols;       /* x: rows x cols; W: vocab x cols; rows <= 2^22, vocab <= 2^21, cols <= 2^16 */
+  int64_t rows, vocab, cols;       /* x: rows x cols; W: vocab x cols; rows <= 2^22, vocab <= 2^21, cols <= 2^16;
+                                      rows x vocab of 2^36 always fits, of more where one launch holds its tiles */
   int32_t dtype;                   /* x, W and their gradients: F32 or BF16 */
   int32_t reduction;               /* adapm_reduction_t */
   float scale;
@@ -295,7 +296,8 @@ adapm_status_t adapm_head_loss(const adapm_head_t* h, adapm_rows_t x, adapm_rows
                                void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* Gradients of upstream * loss (upstream_dev: one float, NULL: 1) by x and W, for the same arguments and the lse of
- * adapm_head_loss.  Either of dx and dweight may have data = NULL; rows that do not count get dx = 0.  All vocab rows of dweight
+ * adapm_head_loss.  Either of dx and dweight may have data = NULL; rows that do not count get dx = 0.  dx may be x; apart from that dx and dweight
+ * overlap neither the inputs nor one another.  All vocab rows of dweight
  * are written: for the output head of a table that buffer is the block's gradient in adapm_step.  bf16: P = w (softmax - onehot) is
  * rounded to bf16 between the products (up to 32 rows, with row weights up to 1024, it is kept as two bf16 numbers). */
 adapm_status_t adapm_head_backward(const adapm_head_t* h, adapm_rows_t x, adapm_rows_t weight, const int64_t* targets_dev,

@@ -5,10 +5,10 @@
 //
 // Forward: a workgroup makes one tile of logits on the matrix cores and leaves only the maximum and the sum of exponentials of its
 // columns for every row; a second launch joins them.  Backward: the vocabulary is taken in pieces; for each, P is made from fresh
-// logits and stored in the type of x (a piece is at most PIECE_BYTES, not the rows x vocab of all logits), then one launch adds
+// logits and stored in the type of x (a piece is about PIECE_BYTES or 2048 vocabulary rows, not the rows x vocab of all logits), then one launch adds
 // its part to dx and writes its rows of dW.  The logits are made twice because keeping them does not pay here: at 1600 columns a
-// logit costs 3.2 kflop, 3 ps of the matrix cores at the rate these kernels reach; to write it in fp32, read it and write P again
-// takes 10 bytes, 2 ps of memory, and as much memory as the operator is there to save.
+// logit costs 3.2 kflop, 2.9 ps of the matrix cores at the rate these kernels reach; to write it in fp32, read it and write P again
+// takes 10 bytes, 2.0 ps of memory, and as much memory as the operator is there to save.
 //
 // Rows without a target are left out before anything else: the rows that count are packed side by side (padded to whole steps of the
 // contraction), so masked rows cost nothing, and whatever stands in them (NaN included) reaches no sum.
@@ -834,12 +834,12 @@ typedef Cfg<float, 2, 2, 4, 1> Small32;       // 128 x 32, four
 
 // A kind of tile: a compute unit runs per_cu workgroups of it and is through with a slice in `share` then; few of them take `lag` more
 struct Shape {
-  int kind, bm, bn, wm, per_cu;
+  int kind, bm, bn, wm, threads, per_cu;
   double share, lag;
 };
 template <class C>
 constexpr Shape shape(int kind, int per_cu, double share, double lag) {
-  return Shape{kind, C::BM, C::BN, C::WM, per_cu, share, lag};
+  return Shape{kind, C::BM, C::BN, C::WM, C::THREADS, per_cu, share, lag};
 }
 constexpr int CUS = 256;
 constexpr double TILE = 4.0;                  // a tile's beginning and end, in slices
@@ -1034,6 +1034,7 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, boo
     const Shape& f = forward_shape(rows > 0 ? rows : 1, vocab, cols, bf16);
     l.kind = f.kind;
     l.tiles = (int)((vocab + f.bm - 1) / f.bm) * f.wm;
+    l.threads = (vocab + f.bm - 1) / f.bm * ((rows + f.bn - 1) / f.bn) * f.threads;
     l.part = take(8 * rows * l.tiles);
     l.hit = take(4 * rows);
     l.sums = take(8 * ((rows + 7) / 8));
@@ -1043,6 +1044,10 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, boo
     l.width = c.width;
     l.splits = c.splits;
     l.dx_first = c.dx_first;
+    const Shape& f = *c.shape;
+    const int64_t logits = (c.width + f.bm - 1) / f.bm * ((rows + f.bn - 1) / f.bn);
+    const int64_t grads = (cols + f.bm - 1) / f.bm * ((c.width + f.bn - 1) / f.bn + (rows2 + f.bn - 1) / f.bn * c.splits);
+    l.threads = (logits > grads ? logits : grads) * f.threads;
     l.p = take(rows2 * c.width * es);
     if (want_dx) l.acc = take(4 * rows2 * pitch * c.splits);
   }

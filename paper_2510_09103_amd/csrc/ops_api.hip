@@ -78,6 +78,9 @@ adapm_status_t check_head(const adapm_head_t* h) {
   return ADAPM_OK;
 }
 
+// The products' tiles are one dimension of a grid, which holds less than 2^32 threads.
+constexpr int64_t GRID_THREADS = 1ll << 32;
+
 // Rows that are whole 16-byte vectors are read where they are; others are copied into the workspace.
 bool in_place(const adapm_head_t* h, const adapm_rows_t& w) {
   const int v = 16 / esize(h->dtype);
@@ -115,6 +118,7 @@ adapm_status_t head_args(const adapm_head_t* h, adapm_rows_t x, adapm_rows_t wei
   d.twin = backward ? head_twin(h->rows, d.bf16, row_weight != nullptr) : 0;
   d.direct = !backward && head_direct(h->rows) && in_place(h, x) && x.stride <= (1ll << 21);
   d.lay = head_layout(h->rows, h->vocab, h->cols, d.bf16, d.w_packed, backward, want_dx, d.twin);
+  if (d.lay.threads >= GRID_THREADS) return fail(ADAPM_EINVAL, "rows %lld x vocab %lld: too many for one call", (long long)h->rows, (long long)h->vocab);
   if (h->rows && workspace_bytes < (size_t)d.lay.bytes)
     return fail(ADAPM_EINVAL, "workspace of %zu bytes, %lld are needed", workspace_bytes, (long long)d.lay.bytes);
   *out = d;
@@ -160,6 +164,7 @@ adapm_status_t adapm_norm_forward(const adapm_norm_t* n, adapm_rows_t x, adapm_r
     if (n->y_dtype == ADAPM_E4M3) TRY(check_ptr("y_scale", y_scale, 4));
   }
   if (!n->rows) return ADAPM_OK;
+  if (y.data == h.data) return fail(ADAPM_EINVAL, "y is h");
   d.rows = n->rows;
   d.cols = (int)n->cols;
   d.eps = n->eps;
@@ -198,6 +203,7 @@ adapm_status_t adapm_norm_backward(const adapm_norm_t* n, adapm_rows_t dy, adapm
   TRY(check_ptr("workspace_dev", workspace_dev, 256));
   NormDev d = {};
   TRY(drop_of(drop, n->rows, n->cols, &d.drop));
+  if (n->rows && d.drop.thr && dx.data == dresidual.data) return fail(ADAPM_EINVAL, "with dropout dx and dresidual differ");
   d.rows = n->rows;
   d.cols = (int)n->cols;
   d.dy = rows_of(dy);
@@ -222,8 +228,9 @@ size_t adapm_head_workspace_bytes(const adapm_head_t* h, adapm_rows_t weight, in
   const bool bf16 = h->dtype == ADAPM_BF16, packed = !in_place(h, weight);
   int64_t bytes = 0;
   for (int weighted = 0; weighted < (backward ? 2 : 1); ++weighted) {
-    const int64_t b = head_layout(h->rows, h->vocab, h->cols, bf16, packed, backward != 0, true, backward ? head_twin(h->rows, bf16, weighted != 0) : 0).bytes;
-    bytes = b > bytes ? b : bytes;
+    const HeadLayout l = head_layout(h->rows, h->vocab, h->cols, bf16, packed, backward != 0, true, backward ? head_twin(h->rows, bf16, weighted != 0) : 0);
+    if (l.threads >= GRID_THREADS) return 0;
+    bytes = l.bytes > bytes ? l.bytes : bytes;
   }
   return (size_t)bytes;
 }
@@ -258,6 +265,9 @@ adapm_status_t adapm_head_backward(const adapm_head_t* h, adapm_rows_t x, adapm_
   if (upstream) TRY(check_ptr("upstream", upstream, 4));
   if (dx.data) TRY(check_rows("dx", dx, h->rows, h->cols, h->dtype));
   if (dweight.data) TRY(check_rows("dweight", dweight, 1, h->cols, h->dtype));
+  // W and the packed x are read while gradients are written
+  if (dweight.data && (dweight.data == weight.data || (h->rows && dweight.data == x.data))) return fail(ADAPM_EINVAL, "dweight is an input");
+  if (dx.data && h->rows && (dx.data == weight.data || dx.data == dweight.data)) return fail(ADAPM_EINVAL, "dx is W or dweight");
   d.lse = const_cast<float*>(lse);
   d.upstream = upstream;
   d.dx = rows_of(dx);

@@ -58,6 +58,7 @@ struct HeadLayout {
   int splits;                                                 // ... parts of dx's contraction over them
   bool dx_first;                                              // ... dx's tiles are given out before dW's
   int64_t bytes;
+  int64_t threads;                                            // of the largest launch of the products
 };
 
 struct HeadDev {

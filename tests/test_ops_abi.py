@@ -58,9 +58,10 @@ def norm(**kw):
     (norm(), dict(residual=OKR, h=B.rows()), "h is null"), (norm(), dict(h=B.rows(), drop=B.adapm_dropout_t(0, 0, None, 0.5, 0)), "h is null"),
     (norm(), dict(h=B.rows(A + 1, 64)), "h is not aligned"), (norm(), dict(weight=0), "weight is null"), (norm(), dict(weight=A + 2), "weight"),
     (norm(), dict(rstd=0), "rstd"), (norm(y_dtype=2), dict(scale=0), "y_scale"), (norm(), dict(drop=B.adapm_dropout_t(0, 0, None, 2.0, 0)), "probability"),
+    (norm(), dict(h=OKR, y=OKR), "y is h"),
 ])
 def test_norm_forward_refusals(n, kw, word):
-    d = dict(x=OKR, residual=B.rows(), h=OKR, weight=A, y=OKR, scale=A, rstd=A, drop=None)
+    d = dict(x=OKR, residual=B.rows(), h=B.rows(2 * A, 64), weight=A, y=OKR, scale=A, rstd=A, drop=None)
     d.update(kw)
     refused(lambda: B.adapm_norm_forward(n, d["x"], d["residual"], d["h"], d["weight"], d["y"], d["scale"], d["rstd"], d["drop"]), word)
 
@@ -70,11 +71,12 @@ def test_norm_forward_refusals(n, kw, word):
     (norm(), dict(h=B.rows()), "h is null"), (norm(), dict(dx=B.rows()), "dx is null"), (norm(), dict(dh=B.rows(A, 1)), "dh: row stride"),
     (norm(), dict(dres=B.rows(A + 1, 64)), "dresidual"), (norm(), dict(dw=0), "dweight"), (norm(), dict(dw=A + 2), "dweight"),
     (norm(), dict(weight=0), "weight"), (norm(), dict(rstd=0), "rstd"), (norm(), dict(ws=0), "workspace"), (norm(), dict(ws=A + 64), "workspace"),
+    (norm(), dict(drop=B.adapm_dropout_t(0, 0, None, 0.5, 0)), "dx and dresidual differ"),
 ])
 def test_norm_backward_refusals(n, kw, word):
-    d = dict(dy=OKR, dh=B.rows(), h=OKR, weight=A, rstd=A, dx=OKR, dres=OKR, dw=A, ws=A)
+    d = dict(dy=OKR, dh=B.rows(), h=OKR, weight=A, rstd=A, dx=OKR, dres=OKR, dw=A, ws=A, drop=None)
     d.update(kw)
-    refused(lambda: B.adapm_norm_backward(n, d["dy"], d["dh"], d["h"], d["weight"], d["rstd"], d["dx"], d["dres"], d["dw"], None, d["ws"]), word)
+    refused(lambda: B.adapm_norm_backward(n, d["dy"], d["dh"], d["h"], d["weight"], d["rstd"], d["dx"], d["dres"], d["dw"], d["drop"], d["ws"]), word)
 
 
 def head(**kw):
@@ -103,10 +105,11 @@ def test_head_loss_refusals(h, kw, word):
 @pytest.mark.parametrize("h,kw,word", [(h, {}, w) for h, w in BAD_HEADS] + [
     (head(), dict(dx=B.rows(), dw=B.rows()), "both null"), (head(), dict(lse=0), "lse"), (head(), dict(up=A + 2), "upstream"),
     (head(), dict(dx=B.rows(A, 1)), "dx: row stride"), (head(), dict(dw=B.rows(A + 1, 64)), "dweight"), (head(), dict(size=0), "are needed"),
-    (head(), dict(t=0), "targets"),
+    (head(), dict(t=0), "targets"), (head(), dict(dw=OKR), "dweight is an input"), (head(), dict(dx=B.rows(5 * A, 64), dw=B.rows(5 * A, 64)), "dx is"),
+    (head(), dict(w=B.rows(3 * A, 64), dw=B.rows(3 * A, 64)), "dweight is an input"), (head(), dict(w=B.rows(3 * A, 64), dx=B.rows(3 * A, 64)), "dx is"),
 ])
 def test_head_backward_refusals(h, kw, word):
-    d = dict(x=OKR, w=OKR, t=A, rw=0, lse=A, up=0, dx=OKR, dw=OKR, ws=A, size=1 << 30)
+    d = dict(x=OKR, w=OKR, t=A, rw=0, lse=A, up=0, dx=B.rows(2 * A, 64), dw=B.rows(4 * A, 64), ws=A, size=1 << 30)
     d.update(kw)
     refused(lambda: B.adapm_head_backward(h, d["x"], d["w"], d["t"], d["rw"], d["lse"], d["up"], d["dx"], d["dw"], d["ws"], d["size"]), word)
 
@@ -124,6 +127,17 @@ def test_workspace_sizes():
     odd = B.adapm_head_workspace_bytes(big, B.rows(A, 1025), True)
     assert odd >= bwd + 50304 * 1024 * 2
     assert B.adapm_head_workspace_bytes(big, B.rows(A + 2, 1024), True) == odd
+
+
+@pytest.mark.parametrize("dtype", [B.ADAPM_BF16, B.ADAPM_F32])
+def test_more_tiles_than_a_launch_holds(dtype):
+    for cols in (64, 1000, 16384):
+        for rows in (1 << 15, 300000, 1 << 22):         # 2^36 logits
+            h, w = head(rows=rows, vocab=(1 << 36) // rows, cols=cols, dtype=dtype), B.rows(A, cols)
+            assert all(B.adapm_head_workspace_bytes(h, w, b) > 0 for b in (False, True))
+        big, x = head(rows=1 << 22, vocab=1 << 21, cols=cols, dtype=dtype), B.rows(A, cols)
+        assert B.adapm_head_workspace_bytes(big, w, False) == 0
+        refused(lambda: B.adapm_head_loss(big, x, w, A, 0, A, A, A, A, 1 << 62), "too many for one call")
 
 
 def test_tensors_are_checked():

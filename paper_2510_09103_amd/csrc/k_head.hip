@@ -7,7 +7,7 @@
 // columns for every row; a second launch joins them.  Backward: the vocabulary is taken in pieces; for each, P is made from fresh
 // logits and stored in the type of x (a piece is about PIECE_BYTES or 2048 vocabulary rows, not the rows x vocab of all logits), then one launch adds
 // its part to dx and writes its rows of dW.  The logits are made twice because keeping them does not pay here: at 1600 columns a
-// logit costs 3.2 kflop, 2.9 ps of the matrix cores at the rate these kernels reach; to write it in fp32, read it and write P again
+// logit costs 3.2 kflop, 2.5 ps of the matrix cores at the rate these kernels reach; to write it in fp32, read it and write P again
 // takes 10 bytes, 2.0 ps of memory, and as much memory as the operator is there to save.
 //
 // Rows without a target are left out before anything else: the rows that count are packed side by side (padded to whole steps of the
@@ -50,8 +50,8 @@ __device__ __forceinline__ float grad_factor(const HeadDev& h, int n) {
 // those near -1 lose little.  With weights on the rows they lose as much as any number, and it is 1.42 times; what a single P has lost
 // averages over the rows that a gradient comes from, or does not where they are few (1.26 times at worst in 40 problems of 32 rows, with
 // weights 1.77; 1.51 of 700 rows, 1.46 of 1500).  The second numbers are more rows of P, against a second copy of x: dW's contraction
-// takes them in, and dx's sums for them are added to those of the first.  32 rows over 32000 x 2048 109 -> 115 us, 512 with weights
-// 229 -> 339.
+// takes them in, and dx's sums for them are added to those of the first.  32 rows over 32000 x 2048 112 -> 120 us, 512 with weights
+// 253 -> 379.
 constexpr int64_t TWIN_ROWS = 32, TWIN_ROWS_WEIGHTED = 1024;
 
 // ---- rows that count -------------------------------------------------------------------------------------------------
@@ -886,9 +886,10 @@ double finish_time(int64_t n1, double l1, int64_t n2, double l2, int64_t slots) 
 
 // The tiles of a piece's gradients are few and unequal: those of dW have the rows of x for their contraction, those of dx the piece's
 // vocabulary, which can be cut, at the price of one more fp32 sum of dx to write and read.  Pieces of equal width, the parts of dx and
-// which tiles come first are chosen by the time that follows from the tiles, for all rows and for two thirds of them: how many count is known on the device alone.  Loss and gradients of 8192 rows over
-// 32000 x 2048 / of 5500 over 32000 x 512, in four pieces of 134 MB 3527 / 1053 us (2 x 32 tiles of dW leave half of the chip idle in the
-// second), in three 3905 / 947, in two 3519 / 899, in one that the last-level cache does not hold 3606 / 872.
+// which tiles come first are chosen by the time that follows from the tiles, for all rows and for two thirds of them: how many count is
+// known on the device alone.  Backward of 8192 rows over 32000 x 512 in 2, 3, 4, 5 pieces 790, 919, 1001, 1164 us (tiles of dW that leave half of
+// the chip idle), with two thirds of the rows 584, 600, 706, 786; over 32000 x 2048 2666, 2889, 2560, 2805 and 1900, 1920, 1903, 2111; over
+// 50257 x 1600 in 4, 5, 6, 8 pieces 3841, 3440, 3711, 3984 and 2628, 2594, 2666, 2633.
 Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, int twin, const Shape& f) {
   const int64_t es = bf16 ? 2 : 4, bk = 128 / es, slots = CUS * f.per_cu;
   const double us_per_byte = 1.0 / 4e6;
@@ -897,7 +898,7 @@ Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, int twin, con
   if (fewest > most) fewest = most;
   const int64_t mt = (cols + f.bm - 1) / f.bm, kd = (cols + bk - 1) / bk;
   Cut best{&f, 0, 1, false, 0.0};
-  for (int64_t p = fewest; p <= most && p <= 4 * fewest; p += (fewest + 1) / 2) {
+  for (int64_t p = fewest; p <= most && p <= 2 * fewest + 3; p += (fewest + 7) / 8) {
     const int64_t width = up((vocab + p - 1) / p, 256), pieces = (vocab + width - 1) / width;
     const int64_t mp = (width + f.bm - 1) / f.bm, tw = mt * ((width + f.bn - 1) / f.bn), kv = width / bk;
     static const int parts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
@@ -921,9 +922,9 @@ Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, int twin, con
   return best;
 }
 
-// Which tiles the passes take: those with the shorter time.  bf16 over 50257 x 1600, small and big tiles, us forward / backward: 64 rows 50 /
-// 150 and 54 / 206, 128 rows 65 / 175 and 58 / 202, 256 rows 85 / 253 and 59 / 230, 1024 rows 218 / 693 and 173 / 568; over 4099 x 256,
-// where big tiles are few, 1024 rows 29 / 40 and 30 / 63.
+// Which tiles the passes take: those with the shorter time.  bf16 over 50257 x 1600, small and big tiles, us forward / backward: 64 rows 45 /
+// 144 and 56 / 183, 128 rows 62 / 179 and 57 / 185, 256 rows 83 / 248 and 58 / 211, 1024 rows 217 / 697 and 173 / 551; over 4099 x 256,
+// where big tiles are few, 1024 rows 24 / 38 and 26 / 59.
 const Shape& forward_shape(int64_t rows, int64_t vocab, int64_t cols, bool bf16) {
   int best = 0;
   double least = 0.0;

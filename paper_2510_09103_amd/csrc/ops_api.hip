@@ -116,7 +116,9 @@ adapm_status_t head_args(const adapm_head_t* h, adapm_rows_t x, adapm_rows_t wei
   d.ws = (char*)const_cast<void*>(workspace);
   d.w_packed = !in_place(h, weight);
   d.twin = backward ? head_twin(h->rows, d.bf16, row_weight != nullptr) : 0;
-  d.direct = !backward && head_direct(h->rows) && in_place(h, x) && x.stride <= (1ll << 21);
+  const bool as_it_is = in_place(h, x) && x.stride <= (1ll << 21);
+  d.direct = !backward && head_direct(h->rows) && as_it_is;
+  d.whole = head_whole(h->rows) && as_it_is;
   d.lay = head_layout(h->rows, h->vocab, h->cols, d.bf16, d.w_packed, backward, want_dx, d.twin);
   if (d.lay.threads >= GRID_THREADS) return fail(ADAPM_EINVAL, "rows %lld x vocab %lld: too many for one call", (long long)h->rows, (long long)h->vocab);
   if (h->rows && workspace_bytes < (size_t)d.lay.bytes)

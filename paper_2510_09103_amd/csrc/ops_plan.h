@@ -75,6 +75,7 @@ struct HeadDev {
   HeadLayout lay;
   int w_packed;
   int direct;                    // forward: x is read where it is
+  int whole;                     // x is read where it is if all of its rows count
   int twin;                      // backward: P as two numbers
 };
 
@@ -83,6 +84,8 @@ int head_twin(int64_t rows, bool bf16, bool weighted);
 
 // whether a forward pass of so many rows reads x where it is, if x's rows are whole aligned vectors
 bool head_direct(int64_t rows);
+// whether a pass of so many rows does, if all of them count
+bool head_whole(int64_t rows);
 
 // backward: whether space for the gradients' pass is wanted (else the forward pass)
 HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx, int twin);

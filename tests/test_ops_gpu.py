@@ -265,6 +265,44 @@ def test_head_strided_operands_and_results(rows, cols, dtype):
     assert part[1] is None and torch.equal(part[0], dx)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,vocab,cols,out", [(1025, 300, 72, 0), (1500, 700, 200, 0), (2100, 513, 64, 1), (1100, 300, 50, 0)])
+def test_head_many_rows_that_all_count(rows, vocab, cols, out, dtype):
+    """Aligned rows that all count are read where they are, at any distance from one another, and dx may replace them."""
+    x, W, t = problem(rows, vocab, cols, dtype, seed=11)
+    t[-1:][:out] = -100
+    r, dx, dW = check_head(x, W, t)
+    wide = torch.full((rows, cols + 24), float("nan"), device="cuda", dtype=dtype)
+    wide[:, 8:cols + 8] = x
+    view = wide[:, 8:cols + 8]
+    again = ops.head_loss(view, W, t)
+    dx2, dW2 = ops.head_backward(view, W, t, again.lse)
+    for a, b in zip((*again, dx2, dW2), (*r, dx, dW)):
+        assert torch.equal(a, b)
+    dx3, dW3 = ops.head_backward(view, W, t, again.lse, dx=view)
+    assert torch.equal(view, dx) and torch.equal(dW3, dW) and wide[:, :8].isnan().all() and wide[:, cols + 8:].isnan().all()
+
+
+def test_head_replays_while_the_rows_that_count_change():
+    x, W, t = problem(1300, 400, 64, BF16, seed=12)
+    keep = t.clone()
+    ops.head_loss(x, W, t)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = ops.head_loss(x, W, t)
+        dx, dW = ops.head_backward(x, W, t, r.lse)
+    for out in (0, 400, 0, 1300, 1, 0):
+        t.copy_(keep)
+        t[:out] = -100
+        graph.replay()
+        torch.cuda.synchronize()
+        want = ops.head_loss(x, W, t)
+        dx2, dW2 = ops.head_backward(x, W, t, want.lse)
+        for a, b in zip((*r, dx, dW), (*want, dx2, dW2)):
+            assert torch.equal(a, b), out
+
+
 @pytest.mark.parametrize("rows,vocab,cols,dtype", [(33000, 2500, 24, BF16), (16400, 2100, 40, F32)])
 def test_head_in_several_pieces(rows, vocab, cols, dtype):
     check_head(*problem(rows, vocab, cols, dtype, 0.1))

@@ -59,6 +59,7 @@ constexpr int64_t TWIN_ROWS = 32, TWIN_ROWS_WEIGHTED = 1024;
 // one that does not count is left out behind the products.
 constexpr int COUNT_ROWS = 1024;                      // rows of a workgroup of the count, and of an entry of its result
 constexpr int PACK_ROWS = 16;                         // rows of a workgroup of the packing
+constexpr int PACK_GROUPS = 512;                      // few rows: up to so many workgroups, which share the columns (16 x 2048 9.7 -> 4.5 us)
 constexpr int DIRECT_ROWS = 32;                       // most rows that are not packed: those that one workgroup joins
 
 __device__ __forceinline__ bool counts(const HeadDev& h, int64_t row) {
@@ -133,8 +134,8 @@ __global__ __launch_bounds__(256) void pack_kernel(HeadDev h) {
     const bool live = in && counts(h, row);
     const unsigned long long m = __ballot(live);
     const int j = before + __popcll(m & ((1ull << threadIdx.x) - 1));
-    if (in) {
-      place[threadIdx.x] = live ? j : -1;
+    if (in) place[threadIdx.x] = live ? j : -1;
+    if (in && blockIdx.y == 0) {
       reinterpret_cast<int*>(h.ws + h.lay.place)[row] = live ? j : -1;
       if (live) {
         reinterpret_cast<int*>(h.ws + h.lay.list)[j] = (int)row;
@@ -146,14 +147,14 @@ __global__ __launch_bounds__(256) void pack_kernel(HeadDev h) {
         h.lse[row] = 0.f;
       }
     }
-    if (threadIdx.x == 0 && r0 + PACK_ROWS >= h.rows) reinterpret_cast<HeadHeader*>(h.ws + h.lay.head)->n = before + __popcll(m);
+    if (threadIdx.x == 0 && blockIdx.y == 0 && r0 + PACK_ROWS >= h.rows) reinterpret_cast<HeadHeader*>(h.ws + h.lay.head)->n = before + __popcll(m);
   }
   __syncthreads();
   if (whole(h, all)) return;
   // pieces of 16 bytes of all the rows at once, whatever alignment x has; zeros behind its columns
   constexpr int V = 16 / sizeof(T);
   const int per = h.pitch / V;
-  for (int i = threadIdx.x; i < PACK_ROWS * per; i += 256) {
+  for (int i = blockIdx.y * 256 + threadIdx.x; i < PACK_ROWS * per; i += 256 * gridDim.y) {
     const int r = i / per, c0 = (i - r * per) * V;
     if (r0 + r >= h.rows || place[r] < 0) continue;
     T* to = reinterpret_cast<T*>(h.ws + h.lay.x) + (int64_t)place[r] * h.pitch + c0;
@@ -799,38 +800,52 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_ke
   }
 }
 
-// dx of every row of x: the parts of its sum added in order, zeros where the row does not count
-template <class T>
+// dx of every row of x: the parts of its sum added in a fixed order, zeros where the row does not count.  SL slices of the threads share the
+// parts: of few rows there are many (16 rows over 32000 x 2048: 4.5 us, 15.5 with one thread for four columns of all parts).
+template <class T, int SL>
 __global__ __launch_bounds__(256) void dx_kernel(HeadDev h, int splits) {
+  constexpr int LANES = 256 / SL;
+  __shared__ f32x4 red[SL > 1 ? SL : 1][SL > 1 ? LANES : 1];
   const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
   const int64_t row = blockIdx.x;
   const int j = reinterpret_cast<const int*>(h.ws + h.lay.place)[row];
   const float f = grad_factor(h, n);
-  T* to = reinterpret_cast<T*>(h.dx.p) + row * h.dx.stride;
+  const int l = threadIdx.x % LANES, w = threadIdx.x / LANES, c = ((int)blockIdx.y * LANES + l) * 4;
   const int64_t part = (h.rows << h.twin) * (int64_t)h.pitch;
-  const float* sum = reinterpret_cast<const float*>(h.ws + h.lay.acc) + (j < 0 ? 0 : (int64_t)j * h.pitch);
-  for (int c = threadIdx.x * 4; c < h.cols; c += 1024) {
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    if (j >= 0) {
-      for (int s = 0; s < splits; ++s) x += *reinterpret_cast<const f32x4*>(sum + s * part + c);
-      if (h.twin)
-        for (int s = 0; s < splits; ++s) x += *reinterpret_cast<const f32x4*>(sum + s * part + (int64_t)n * h.pitch + c);
+  const float* sum = reinterpret_cast<const float*>(h.ws + h.lay.acc) + (j < 0 ? 0 : (int64_t)j * h.pitch) + c;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  if (j >= 0 && c < h.cols) {
+#pragma unroll 4
+    for (int s = w; s < splits; s += SL) x += *reinterpret_cast<const f32x4*>(sum + s * part);
+    if (h.twin) {
+      sum += (int64_t)n * h.pitch;
+#pragma unroll 4
+      for (int s = w; s < splits; s += SL) x += *reinterpret_cast<const f32x4*>(sum + s * part);
     }
-    x *= f;
-    if (c + 4 <= h.cols) {
-      if (sizeof(T) == 2) {
-        u32x2 w;
-        w[0] = pack_bf16x2(x[0], x[1]);
-        w[1] = pack_bf16x2(x[2], x[3]);
-        *reinterpret_cast<u32x2_e2*>(to + c) = w;
-      } else {
-        *reinterpret_cast<f32x4_e4*>(to + c) = x;
-      }
-    } else {
+  }
+  if (SL > 1) {
+    red[w][l] = x;
+    __syncthreads();
+    if (w) return;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (c + e < h.cols) to[c + e] = sizeof(T) == 2 ? (T)pack_bf16x2(x[e], 0.f) : (T)x[e];
+    for (int s = 1; s < SL; ++s) x += red[s][l];
+  }
+  if (c >= h.cols) return;
+  T* to = reinterpret_cast<T*>(h.dx.p) + row * h.dx.stride;
+  x *= f;
+  if (c + 4 <= h.cols) {
+    if (sizeof(T) == 2) {
+      u32x2 v;
+      v[0] = pack_bf16x2(x[0], x[1]);
+      v[1] = pack_bf16x2(x[2], x[3]);
+      *reinterpret_cast<u32x2_e2*>(to + c) = v;
+    } else {
+      *reinterpret_cast<f32x4_e4*>(to + c) = x;
     }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < h.cols) to[c + e] = sizeof(T) == 2 ? (T)pack_bf16x2(x[e], 0.f) : (T)x[e];
   }
 }
 
@@ -999,10 +1014,17 @@ void gradients(const HeadDev& h, int64_t width, int splits, hipStream_t s) {
   }
 }
 
+template <class T>
+void joined(const HeadDev& h, int splits, hipStream_t s) {
+  if (splits < 8) hipLaunchKernelGGL((dx_kernel<T, 1>), dim3((unsigned)h.rows, (unsigned)((h.cols + 1023) / 1024)), dim3(256), 0, s, h, splits);
+  else hipLaunchKernelGGL((dx_kernel<T, 8>), dim3((unsigned)h.rows, (unsigned)((h.cols + 127) / 128)), dim3(256), 0, s, h, splits);
+}
+
 void pack_x(const HeadDev& h, hipStream_t s) {
   if (h.rows > COUNT_ROWS)
     hipLaunchKernelGGL(count_kernel, dim3((unsigned)((h.rows + COUNT_ROWS - 1) / COUNT_ROWS)), dim3(256), 0, s, h);
-  const dim3 grid((unsigned)((h.rows + PACK_ROWS - 1) / PACK_ROWS));
+  const int64_t sets = (h.rows + PACK_ROWS - 1) / PACK_ROWS, turns = (PACK_ROWS * (int64_t)h.pitch * (h.bf16 ? 2 : 4) / 16 + 255) / 256;
+  const dim3 grid((unsigned)sets, (unsigned)(sets * turns <= PACK_GROUPS ? turns : sets < PACK_GROUPS ? PACK_GROUPS / sets : 1));
   if (h.bf16) hipLaunchKernelGGL((pack_kernel<uint16_t>), grid, dim3(256), 0, s, h);
   else hipLaunchKernelGGL((pack_kernel<float>), grid, dim3(256), 0, s, h);
 }
@@ -1080,7 +1102,7 @@ void launch_head_loss(const HeadDev& h, hipStream_t s) {
     case 3: logits<Big32>(h, s); break;
     default: logits<Small32>(h, s); break;
   }
-  const int tiles = h.lay.tiles, rl = h.rows <= 8 ? 8 : h.direct ? DIRECT_ROWS : h.rows <= 2048 ? 8 : 16, groups = (int)((h.rows + rl - 1) / rl);
+  const int tiles = h.lay.tiles, rl = h.rows <= 8 ? 8 : h.direct ? (h.rows <= 16 ? 16 : DIRECT_ROWS) : h.rows <= 2048 ? 8 : 16, groups = (int)((h.rows + rl - 1) / rl);
   const dim3 grid((unsigned)groups), block(1024);
   const int last = groups == 1 ? 1 : 0;
   if (rl == 8) hipLaunchKernelGGL((finish_kernel<8>), grid, block, 0, s, h, tiles, last);
@@ -1106,8 +1128,8 @@ void launch_head_backward(const HeadDev& h, hipStream_t s) {
     default: gradients<Small32>(h, width, splits, s); break;
   }
   if (h.dx.p) {
-    if (h.bf16) hipLaunchKernelGGL((dx_kernel<uint16_t>), dim3((unsigned)h.rows), dim3(256), 0, s, h, splits);
-    else hipLaunchKernelGGL((dx_kernel<float>), dim3((unsigned)h.rows), dim3(256), 0, s, h, splits);
+    if (h.bf16) joined<uint16_t>(h, splits, s);
+    else joined<float>(h, splits, s);
   }
 }
 

@@ -11,7 +11,7 @@
 // takes 10 bytes, 2.0 ps of memory, and as much memory as the operator is there to save.
 //
 // Rows without a target are left out before anything else: the rows that count are packed side by side (padded to whole steps of the
-// contraction), so masked rows cost nothing, and whatever stands in them (NaN included) reaches no sum.
+// contraction; where all count and lie well, x itself is read), so masked rows cost nothing, and whatever stands in them (NaN included) reaches no sum.
 #include "ew_math.h"
 #include "ops_plan.h"
 

@@ -60,7 +60,8 @@ constexpr int64_t TWIN_ROWS = 32, TWIN_ROWS_WEIGHTED = 1024;
 constexpr int COUNT_ROWS = 1024;                      // rows of a workgroup of the count, and of an entry of its result
 constexpr int PACK_ROWS = 16;                         // rows of a workgroup of the packing
 constexpr int PACK_GROUPS = 512;                      // few rows: up to so many workgroups, which share the columns (16 x 2048 9.7 -> 4.5 us)
-constexpr int DIRECT_ROWS = 32;                       // most rows that are not packed: those that one workgroup joins
+constexpr int DIRECT_ROWS = 256;                      // most rows that are not packed: a tile's, W is what they cost
+constexpr int JOINED_ROWS = 32;                       // most of them that one workgroup joins, which leaves the loss itself
 
 __device__ __forceinline__ bool counts(const HeadDev& h, int64_t row) {
   const int64_t t = h.targets[row];
@@ -595,7 +596,7 @@ __global__ __launch_bounds__(1024) void finish_kernel(HeadDev h, int tiles, int 
   double part_loss = 0.0;
   int counted = n;
   bool in = w == 0 && row < n;
-  if (h.direct) {                                      // one workgroup
+  if (h.direct) {                                      // counted: of interest where this is the one workgroup
     const bool live = in && counts(h, row);
     if (in && !live) {
       h.lse[row] = 0.f;
@@ -622,10 +623,12 @@ __global__ __launch_bounds__(1024) void finish_kernel(HeadDev h, int tiles, int 
 
 __global__ __launch_bounds__(256) void total_kernel(HeadDev h, int groups) {
   __shared__ double red[256];
-  const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
   const double* sums = reinterpret_cast<const double*>(h.ws + h.lay.sums);
   double s = 0.0;
   for (int i = threadIdx.x; i < groups; i += 256) s += sums[i];
+  static_assert(DIRECT_ROWS <= 256, "a thread each");
+  const int n = h.direct ? __syncthreads_count((int64_t)threadIdx.x < h.rows && counts(h, threadIdx.x))
+                         : reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
   red[threadIdx.x] = s;
   __syncthreads();
   for (int o = 128; o > 0; o >>= 1) {
@@ -1102,12 +1105,12 @@ void launch_head_loss(const HeadDev& h, hipStream_t s) {
     case 3: logits<Big32>(h, s); break;
     default: logits<Small32>(h, s); break;
   }
-  const int tiles = h.lay.tiles, rl = h.rows <= 8 ? 8 : h.direct ? (h.rows <= 16 ? 16 : DIRECT_ROWS) : h.rows <= 2048 ? 8 : 16, groups = (int)((h.rows + rl - 1) / rl);
+  const int tiles = h.lay.tiles, rl = h.rows <= 8 ? 8 : h.direct && h.rows <= JOINED_ROWS ? (h.rows <= 16 ? 16 : JOINED_ROWS) : h.rows <= 2048 ? 8 : 16, groups = (int)((h.rows + rl - 1) / rl);
   const dim3 grid((unsigned)groups), block(1024);
   const int last = groups == 1 ? 1 : 0;
   if (rl == 8) hipLaunchKernelGGL((finish_kernel<8>), grid, block, 0, s, h, tiles, last);
   else if (rl == 16) hipLaunchKernelGGL((finish_kernel<16>), grid, block, 0, s, h, tiles, last);
-  else hipLaunchKernelGGL((finish_kernel<DIRECT_ROWS>), grid, block, 0, s, h, tiles, last);
+  else hipLaunchKernelGGL((finish_kernel<JOINED_ROWS>), grid, block, 0, s, h, tiles, last);
   if (!last) hipLaunchKernelGGL(total_kernel, dim3(1), dim3(256), 0, s, h, groups);
 }
 

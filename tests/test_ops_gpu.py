@@ -220,7 +220,7 @@ def test_head(rows, vocab, cols, dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,vocab,cols,masked", [(1, 50, 16, 1.0), (6, 200, 64, 0.5), (20, 333, 72, 0.5), (32, 90, 40, 1.0), (40, 333, 24, 0.5), (400, 600, 64, 0.9), (1300, 700, 40, 0.4),
-                                                    (2100, 130, 72, 1.0), (1500, 257, 33, 0.02)])
+                                                    (2100, 130, 72, 1.0), (1500, 257, 33, 0.02), (33, 300, 64, 1.0), (200, 5000, 128, 0.3), (256, 129, 64, 0.5), (257, 600, 40, 0.5)])
 def test_head_rows_without_a_target(rows, vocab, cols, masked, dtype):
     x, W, t = problem(rows, vocab, cols, dtype, masked, seed=3)
     out = (t < 0) | (t >= vocab)

@@ -50,8 +50,8 @@ __device__ __forceinline__ float grad_factor(const HeadDev& h, int n) {
 // those near -1 lose little.  With weights on the rows they lose as much as any number, and it is 1.42 times; what a single P has lost
 // averages over the rows that a gradient comes from, or does not where they are few (1.26 times at worst in 40 problems of 32 rows, with
 // weights 1.77; 1.51 of 700 rows, 1.46 of 1500).  The second numbers are more rows of P, against a second copy of x: dW's contraction
-// takes them in, and dx's sums for them are added to those of the first.  32 rows over 32000 x 2048 112 -> 120 us, 512 with weights
-// 253 -> 379.
+// takes them in, and dx's sums for them are added to those of the first.  32 rows over 32000 x 2048 101 -> 104 us, 512 with weights
+// 253 -> 372.
 constexpr int64_t TWIN_ROWS = 32, TWIN_ROWS_WEIGHTED = 1024;
 
 // ---- rows that count -------------------------------------------------------------------------------------------------
@@ -873,8 +873,8 @@ constexpr int CUS = 256;
 constexpr double TILE = 4.0;                  // a tile's beginning and end, in slices
 constexpr Shape SHAPES[5] = {shape<Big>(0, 1, 1.57, 0.0), shape<Small>(1, 3, 0.285, 0.45), shape<Thin>(2, 2, 0.25, 0.2),
                              shape<Big32>(3, 2, 1.95, 0.0), shape<Small32>(4, 4, 0.58, 0.0)};
-// Those for a type.  Thin is for the forward pass of rows that are one of its tiles, where reading W is all: one row over 32000 x 2048 33
-// us, 36 with Small; the products of the backward pass gain nothing from it.
+// Those for a type.  Thin is for the forward pass of rows that are one of its tiles, where reading W is all: one row over 32000 x 2048 27
+// us, 29 with Small (W in the last-level cache); the products of the backward pass gain nothing from it.
 int first_shape(bool bf16) { return bf16 ? 0 : 3; }
 int end_shape(bool bf16, bool thin) { return !bf16 ? 5 : thin ? 3 : 2; }
 
@@ -950,9 +950,9 @@ Cut cut_with(int64_t rows, int64_t vocab, int64_t cols, bool bf16, int twin, con
   return best;
 }
 
-// Which tiles the passes take: those with the shorter time.  bf16 over 50257 x 1600, small and big tiles, us forward / backward: 64 rows 45 /
-// 144 and 56 / 183, 128 rows 62 / 179 and 57 / 185, 256 rows 83 / 248 and 58 / 211, 1024 rows 217 / 697 and 173 / 551; over 4099 x 256,
-// where big tiles are few, 1024 rows 24 / 38 and 26 / 59.
+// Which tiles the passes take: those with the shorter time.  bf16 over 50257 x 1600, small and big tiles, us forward / backward: 64 rows 37 /
+// 131 and 48 / 166, 128 rows 56 / 170 and 49 / 174, 256 rows 76 / 243 and 49 / 199, 1024 rows 223 / 702 and 169 / 549; over 4099 x 256,
+// where big tiles are few, 1024 rows 24 / 38 and 26 / 58.
 const Shape& forward_shape(int64_t rows, int64_t vocab, int64_t cols, bool bf16) {
   int best = 0;
   double least = 0.0;

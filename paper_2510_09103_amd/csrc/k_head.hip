@@ -33,7 +33,6 @@ typedef __attribute__((address_space(3))) unsigned char lds_u8;
 constexpr unsigned OOB = 0x80000000u;                 // an offset past every descriptor's end: reads zeros
 constexpr int64_t PIECE_BYTES = (int64_t)256 << 20;   // most of P at a time: the size of the last-level cache
 constexpr float LOG2E = 1.44269504088896340736f;
-constexpr float LOG2E_LOW = (float)(1.44269504088896340736 - (double)LOG2E);
 
 struct HeadHeader {
   int n;                                              // rows that count
@@ -528,9 +527,10 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void logits_
       for (int e = 0; e < 4; ++e) top = fmaxf(top, acc.v[i][j][e]);
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    // exp(s - top) = 2^(s log2 e - c) 2^-rest with c = top log2 e rounded: one multiply-add an element, and what the rounding of c has
-    // left out goes into the sum once.  A wave without a column of the vocabulary leaves (-inf, 0).
-    const float c = top == -INFINITY ? 0.f : top * LOG2E, rest = top == -INFINITY ? 0.f : fmaf(top, LOG2E, -c) + top * LOG2E_LOW;
+    // exp(s - top) = 2^(s L - c) 2^-rest with L = log2 e as fp32, c = top L rounded, rest = top L - c: one multiply-add an element, and what
+    // the rounding of c has left out goes into the sum once.  The elements and the rest have the same L, so the top's element is 1 at any
+    // size of the logits, and what L leaves out of log2 e (1.9e-8) meets s - top alone.  A wave without a column of the vocabulary leaves (-inf, 0).
+    const float c = top == -INFINITY ? 0.f : top * LOG2E, rest = top == -INFINITY ? 0.f : fmaf(top, LOG2E, -c);
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < C::MT; ++i)

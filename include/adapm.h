@@ -256,8 +256,8 @@ typedef struct {
 
 /* h = residual + dropout(x) in dtype, rstd = 1 / sqrt(mean(h^2) + eps) (fp32, one a row), y = h * rstd * weight.
  * residual.data and drop may be NULL; with neither, h.data may be NULL and the h of the backward pass is x itself.
- * y_dtype = ADAPM_E4M3: y holds 8-bit values and y_scale[row] = max|row| / 448 (1 for a row of zeros; NaN does not count)
- * is what they are multiplied by.  h may be x or residual; y overlaps none of the others. */
+ * y_dtype = ADAPM_E4M3: y holds 8-bit values and y_scale[row] = max|row| / 448 (1 for a row of zeros, at least 2^-126 for any
+ * other; NaN does not count) is what they are multiplied by.  h may be x or residual; y overlaps none of the others. */
 adapm_status_t adapm_norm_forward(const adapm_norm_t* n, adapm_rows_t x, adapm_rows_t residual, adapm_rows_t h,
                                   const void* weight_dev, adapm_rows_t y, float* y_scale_dev, float* rstd_dev,
                                   const adapm_dropout_t* drop, void* stream);

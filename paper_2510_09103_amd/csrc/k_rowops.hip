@@ -236,7 +236,8 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_forward_kernel(NormDev a
     }
   }
   if (!a.out8) return;
-  // e4m3 with one scale a row: the row's largest value becomes the type's largest, 448
+  // e4m3 with one scale a row: the row's largest value becomes the type's largest, 448.  The scale is a normal number: below 2^-126 the
+  // quotient would lose digits, 1 / scale would be infinite and the row's zeros NaN.  Such a row keeps values of 2^-126 times the type's.
   float top = 0.f;
 #pragma unroll
   for (int k = 0; k < NV; ++k)
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_forward_kernel(NormDev a
         if ((k * TPR + t) * 8 + i < a.cols) top = fmaxf(top, fabsf(h[k].v[i]));
     }
   top = row_max<TPR>(top, red[1]);
-  const float scale = top > 0.f ? top / 448.f : 1.f, inv = 1.f / scale;
+  const float scale = top > 0.f ? fmaxf(top / 448.f, 0x1p-126f) : 1.f, inv = 1.f / scale;
   if (t == 0) a.y_scale[row] = scale;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {

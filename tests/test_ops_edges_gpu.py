@@ -40,3 +40,28 @@ def test_sure_rows_keep_the_digits_of_their_loss(rows, vocab, dtype):
     off = 2 * 2.0 ** -23 + 3 * 2.0 ** -24
     assert float((got - want).abs().max()) <= off, (got - want).tolist()
     R.within("lse", r.lse.cpu(), torch.tensor([top for top, _ in pairs], dtype=torch.float64)[i] + want, off)
+
+
+# ---- norm --------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("cols", [9, 64, 700, 2048, 5000])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_8_bit_rows_near_nothing(cols, dtype):
+    """Rows whose largest value is below what 1 / scale can bring to 448, zeros among them (dropout leaves such)."""
+    x = randn(9, cols, seed=1, dtype=dtype)
+    x[:, 1::3] = 0
+    w = torch.tensor([1e-30, 1e-34, 1e-36, 1e-37, 1e-38, 1e-40, 1e-43, 1e-45, 0.0], device="cuda")
+    for i in range(9):
+        g = w[i].expand(cols).contiguous()
+        n = ops.rms_norm(x[i:i + 1], g, eps=1e-5, out_dtype=E4M3)
+        y = R.norm(n.h, g, 1e-5)[0]
+        top = y.abs().amax().item()
+        want = max(top / 448, 2.0 ** -126) if top > 2.0 ** -150 else 1.0
+        scale = n.scale.double().item()
+        # products of the row's values: 48 roundings, and steps of 2^-149 where they are below the type's normal numbers
+        assert abs(scale - want) <= 48 * R.U * want + 2.0 ** -149, (i, scale, want)
+        got = n.y.to(F32).double() * scale
+        assert bool(torch.isfinite(got).all()) and not bool(got[0, 1::3].any())
+        off = 2.0 ** -4 * y.abs() + 2.0 ** -10 * scale + 60 * R.U * (y.abs() + scale) + 2.0 ** -149
+        if top > 2.0 ** -150:
+            assert bool(((got - y).abs() <= off).all()), (i, float(((got - y).abs() - off).max()))

@@ -296,7 +296,8 @@ adapm_status_t adapm_head_loss(const adapm_head_t* h, adapm_rows_t x, adapm_rows
                                void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* Gradients of upstream * loss (upstream_dev: one float, NULL: 1) by x and W, for the same arguments and the lse of
- * adapm_head_loss.  Either of dx and dweight may have data = NULL; rows that do not count get dx = 0.  dx may be x; apart from that dx and dweight
+ * adapm_head_loss.  Either of dx and dweight may have data = NULL; rows that do not count get dx = 0, and dweight is 0 if
+ * none does, whatever upstream is (inf and NaN too).  dx may be x; apart from that dx and dweight
  * overlap neither the inputs nor one another.  All vocab rows of dweight
  * are written: for the output head of a table that buffer is the block's gradient in adapm_step.  bf16: P = w (softmax - onehot) is
  * rounded to bf16 between the products (up to 32 rows, with row weights up to 1024, it is kept as two bf16 numbers). */

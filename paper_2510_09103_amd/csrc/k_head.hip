@@ -39,9 +39,11 @@ struct HeadHeader {
   int pad[63];
 };
 
+// n: rows that count; without any the gradients are zeros, whatever the upstream gradient (infinite or NaN where a loss scale overflowed)
 __device__ __forceinline__ float grad_factor(const HeadDev& h, int n) {
-  float f = h.scale * (h.upstream ? *h.upstream : 1.f);
-  return h.mean ? f / (float)(n > 0 ? n : 1) : f;
+  if (n == 0) return 0.f;
+  const float f = h.scale * (h.upstream ? *h.upstream : 1.f);
+  return h.mean ? f / (float)n : f;
 }
 
 // Few rows: P travels as two bf16 numbers, P rounded and what that has left out, 2^-17 of it in all.  A gradient in bf16 has an error of
@@ -812,7 +814,7 @@ __global__ __launch_bounds__(256) void dx_kernel(HeadDev h, int splits) {
   const int n = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
   const int64_t row = blockIdx.x;
   const int j = reinterpret_cast<const int*>(h.ws + h.lay.place)[row];
-  const float f = grad_factor(h, n);
+  const float f = j < 0 ? 0.f : grad_factor(h, n);      // zeros times infinity are none
   const int l = threadIdx.x % LANES, w = threadIdx.x / LANES, c = ((int)blockIdx.y * LANES + l) * 4;
   const int64_t part = (h.rows << h.twin) * (int64_t)h.pitch;
   const float* sum = reinterpret_cast<const float*>(h.ws + h.lay.acc) + (j < 0 ? 0 : (int64_t)j * h.pitch) + c;

@@ -42,6 +42,23 @@ def test_sure_rows_keep_the_digits_of_their_loss(rows, vocab, dtype):
     R.within("lse", r.lse.cpu(), torch.tensor([top for top, _ in pairs], dtype=torch.float64)[i] + want, off)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,out", [(6, 3), (40, 11), (1300, 500), (20, 20), (1300, 1300)])
+@pytest.mark.parametrize("factor", [float("inf"), float("nan"), 3e38])
+def test_rows_that_do_not_count_have_no_gradient_whatever_the_factor(rows, out, factor, dtype):
+    """A loss scaler that overflows: rows that do not count get zeros all the same, and so does dweight if no row counts."""
+    x, W = randn(rows, 72, seed=1, dtype=dtype), randn(130, 72, seed=2, dtype=dtype)
+    t = torch.arange(rows, device="cuda") % 130
+    t[:out] = -100
+    lse = ops.head_loss(x, W, t).lse
+    dx, dW = ops.head_backward(x, W, t, lse, scale=4.0, upstream=torch.tensor(factor, device="cuda"))
+    assert not bool(dx[:out].any())
+    if out == rows:
+        assert not bool(dW.any())
+    else:
+        assert not bool(torch.isfinite(dx[out:]).all())
+
+
 # ---- norm --------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("cols", [9, 64, 700, 2048, 5000])

@@ -300,7 +300,8 @@ adapm_status_t adapm_head_loss(const adapm_head_t* h, adapm_rows_t x, adapm_rows
  * none does, whatever upstream is (inf and NaN too).  dx may be x; apart from that dx and dweight
  * overlap neither the inputs nor one another.  All vocab rows of dweight
  * are written: for the output head of a table that buffer is the block's gradient in adapm_step.  bf16: P = w (softmax - onehot) is
- * rounded to bf16 between the products (up to 32 rows, with row weights up to 1024, it is kept as two bf16 numbers). */
+ * rounded to bf16 between the products, which makes the gradients' error 1.07 times that of their own rounding (root mean square), with
+ * row weights 1.42 times.  Where up to 32 rows count, with row weights up to 1024, P is kept as two bf16 numbers: 1.00 times. */
 adapm_status_t adapm_head_backward(const adapm_head_t* h, adapm_rows_t x, adapm_rows_t weight, const int64_t* targets_dev,
                                    const float* row_weight_dev, const float* lse_dev, const float* upstream_dev,
                                    adapm_rows_t dx, adapm_rows_t dweight, void* workspace_dev, size_t workspace_bytes,

@@ -46,14 +46,17 @@ __device__ __forceinline__ float grad_factor(const HeadDev& h, int n) {
   return h.mean ? f / (float)n : f;
 }
 
-// Few rows: P travels as two bf16 numbers, P rounded and what that has left out, 2^-17 of it in all.  A gradient in bf16 has an error of
-// its own, 1.7e-3 of it in root mean square.  P rounded once brings that to 1.2 times as much: the targets' elements are most of it, and
-// those near -1 lose little.  With weights on the rows they lose as much as any number, and it is 1.42 times; what a single P has lost
-// averages over the rows that a gradient comes from, or does not where they are few (1.26 times at worst in 40 problems of 32 rows, with
-// weights 1.77; 1.51 of 700 rows, 1.46 of 1500).  The second numbers are more rows of P, against a second copy of x: dW's contraction
-// takes them in, and dx's sums for them are added to those of the first.  32 rows over 32000 x 2048 101 -> 104 us, 512 with weights
-// 253 -> 372.
-constexpr int64_t TWIN_ROWS = 32, TWIN_ROWS_WEIGHTED = 1024;
+// Few rows that count: P travels as two bf16 numbers, P rounded and what that has left out, 2^-17 of it in all.  A gradient in bf16 has an
+// error of its own, 1.66e-3 of it in root mean square.  P rounded once adds another, most of it from one element a row, the target's, and it
+// does not average out over the rows: from 33 to 4096 of them the whole is 1.07 times the least without weights (the targets' elements
+// near -1 lose little) and 1.42 times with weights on the rows (w (p - 1) loses as much as any number); 1.26 and 1.77 at worst in 40 problems
+// of 32 rows.  Two numbers leave 1.00.  Where they end is a matter of time: the second numbers are more rows of P, against a second copy
+// of x; dW's contraction takes them in, and dx's sums for them are added to those of the first.  Up to 32 rows reading W covers that (32000 x
+// 2048, 32 rows with two numbers 96 us, 33 with one 96).  With weights, where they gain most, they are taken up to 1024 rows (512 rows 347 us
+// against 224, 1024 rows 620 against 398); beyond, where the products are all of the time, a batch is not made half as long again for them.
+// How many rows count is known on the device alone: there is space for the second numbers of up to that many in any batch.
+constexpr int TWIN_ROWS = 32, TWIN_ROWS_WEIGHTED = 1024;
+__device__ __forceinline__ int twin(const HeadDev& h, int n) { return n > 0 && n <= h.twin_rows ? 1 : 0; }
 
 // ---- rows that count -------------------------------------------------------------------------------------------------
 // The few rows of a forward pass whose x can be read where it is are not packed (h.direct): each has a column of logits to itself, and
@@ -72,6 +75,7 @@ __device__ __forceinline__ bool counts(const HeadDev& h, int64_t row) {
 // Many rows that all count, as in pre-training, are not copied either: how many count is known before the packing.  8192 rows over
 // 32000 x 2048, loss and gradients, 3487 -> 3445 us.
 __device__ __forceinline__ bool whole(const HeadDev& h, int n) { return h.whole && n == h.rows; }
+static_assert(TWIN_ROWS <= COUNT_ROWS && TWIN_ROWS_WEIGHTED <= COUNT_ROWS, "rows that are read where they are have no second copy");
 
 __device__ __forceinline__ int live_rows(const HeadDev& h) {
   return h.direct ? (int)h.rows : reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n;
@@ -120,10 +124,11 @@ __global__ __launch_bounds__(256) void pack_kernel(HeadDev h) {
   const int* counted = reinterpret_cast<const int*>(h.ws + h.lay.counts);
   for (int64_t i = threadIdx.x; i < b0; i += 256) c += counted[i];
   for (int64_t row = b0 * COUNT_ROWS + threadIdx.x; row < r0; row += 256) c += counts(h, row) ? 1 : 0;
-  if (h.whole)
+  if (h.rows > COUNT_ROWS) {
     for (int64_t i = threadIdx.x; i * COUNT_ROWS < h.rows; i += 256) c += counted[i] * ONE_OF_ALL;
-  if (h.twin)          // few rows
+  } else if (h.twin_rows) {
     for (int64_t row = threadIdx.x; row < h.rows; row += 256) c += counts(h, row) ? ONE_OF_ALL : 0;
+  }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) c += __shfl_xor(c, o);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
@@ -162,7 +167,7 @@ __global__ __launch_bounds__(256) void pack_kernel(HeadDev h) {
     T* to = reinterpret_cast<T*>(h.ws + h.lay.x) + (int64_t)place[r] * h.pitch + c0;
     const u32x4 v = piece_of(reinterpret_cast<const T*>(h.x.p) + (r0 + r) * h.x.stride, c0, h.cols);
     *reinterpret_cast<u32x4*>(to) = v;
-    if (h.twin) *reinterpret_cast<u32x4*>(to + (int64_t)all * h.pitch) = v;
+    if (twin(h, all)) *reinterpret_cast<u32x4*>(to + (int64_t)all * h.pitch) = v;
   }
 }
 
@@ -704,7 +709,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void piece_k
 #pragma unroll
           for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(p[i + e / 2][2 * (e & 1)], p[i + e / 2][2 * (e & 1) + 1]);
           *reinterpret_cast<u32x4*>(to) = w;
-          if (h.twin) {
+          if (twin(h, n)) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               w[e] = pack_bf16x2(p[i + e / 2][2 * (e & 1)] - bf16lo(w[e]), p[i + e / 2][2 * (e & 1) + 1] - bf16hi(w[e]));
@@ -735,7 +740,7 @@ template <class C>
 __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_kernel(HeadDev h, GradPlan g) {
   typedef typename C::T T;
   HEAD_BUFFERS
-  const int live = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n, n = live << h.twin;      // rows of P and of packed x
+  const int live = reinterpret_cast<const HeadHeader*>(h.ws + h.lay.head)->n, n = live << twin(h, live);      // rows of P and of packed x
   const char* P = h.ws + h.lay.p;
   const int64_t pp = g.pitch * (int64_t)sizeof(T);
   const int n_dw = g.mt * g.nt_w;
@@ -789,7 +794,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_ke
   W.u = cols;
   W.k = g.width;
   product<C, false, true>(W, Src{P, pp, n, (int)g.pitch}, m0, n0, k0, k1, lds, acc);
-  float* sum = reinterpret_cast<float*>(h.ws + h.lay.acc) + (int64_t)split * (h.rows << h.twin) * h.pitch;
+  float* sum = reinterpret_cast<float*>(h.ws + h.lay.acc) + (int64_t)split * h.lay.p_rows * h.pitch;
 #pragma unroll
   for (int j = 0; j < C::NT; ++j) {
     const int row = n0 + un + 16 * j + l16;
@@ -816,13 +821,13 @@ __global__ __launch_bounds__(256) void dx_kernel(HeadDev h, int splits) {
   const int j = reinterpret_cast<const int*>(h.ws + h.lay.place)[row];
   const float f = j < 0 ? 0.f : grad_factor(h, n);      // zeros times infinity are none
   const int l = threadIdx.x % LANES, w = threadIdx.x / LANES, c = ((int)blockIdx.y * LANES + l) * 4;
-  const int64_t part = (h.rows << h.twin) * (int64_t)h.pitch;
+  const int64_t part = h.lay.p_rows * (int64_t)h.pitch;
   const float* sum = reinterpret_cast<const float*>(h.ws + h.lay.acc) + (j < 0 ? 0 : (int64_t)j * h.pitch) + c;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
   if (j >= 0 && c < h.cols) {
 #pragma unroll 4
     for (int s = w; s < splits; s += SL) x += *reinterpret_cast<const f32x4*>(sum + s * part);
-    if (h.twin) {
+    if (twin(h, n)) {
       sum += (int64_t)n * h.pitch;
 #pragma unroll 4
       for (int s = w; s < splits; s += SL) x += *reinterpret_cast<const f32x4*>(sum + s * part);
@@ -883,7 +888,7 @@ int end_shape(bool bf16, bool thin) { return !bf16 ? 5 : thin ? 3 : 2; }
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 }  // namespace
-int head_twin(int64_t rows, bool bf16, bool weighted) { return bf16 && rows <= (weighted ? TWIN_ROWS_WEIGHTED : TWIN_ROWS) ? 1 : 0; }
+int head_twin_rows(bool bf16, bool weighted) { return !bf16 ? 0 : weighted ? TWIN_ROWS_WEIGHTED : TWIN_ROWS; }
 namespace {
 
 // How the backward pass is cut.
@@ -1007,7 +1012,7 @@ void gradients(const HeadDev& h, int64_t width, int splits, hipStream_t s) {
     g.width = (int)(h.vocab - first < width ? h.vocab - first : width);
     g.pitch = width;
     const int mp = (int)((up(g.width, 64) + C::BM - 1) / C::BM), np = (int)((h.rows + C::BN - 1) / C::BN);
-    const int nx = (int)(((h.rows << h.twin) + C::BN - 1) / C::BN);
+    const int nx = (int)((h.lay.p_rows + C::BN - 1) / C::BN);
     hipLaunchKernelGGL((piece_kernel<C>), dim3((unsigned)(mp * np)), dim3(C::THREADS), 0, s, h, first, g.width, width, mp);
     g.mt = (h.cols + C::BM - 1) / C::BM;
     g.splits = h.dx.p ? splits : 0;
@@ -1046,9 +1051,11 @@ void pack(const HeadDev& h, hipStream_t s) {
 bool head_direct(int64_t rows) { return rows <= DIRECT_ROWS; }
 bool head_whole(int64_t rows) { return rows > COUNT_ROWS; }
 
-HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx, int twin) {
-  const int64_t es = bf16 ? 2 : 4, pitch = up(cols, bf16 ? 64 : 32), rows2 = rows << twin;
+HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx, int twin_rows) {
+  // up to twin_rows of them twice, or all of them once
+  const int64_t es = bf16 ? 2 : 4, pitch = up(cols, bf16 ? 64 : 32), twice = 2 * (rows < twin_rows ? rows : twin_rows), rows2 = rows > twice ? rows : twice;
   HeadLayout l;
+  l.p_rows = rows2;
   l.width = 0;
   l.splits = 0;
   l.dx_first = false;
@@ -1078,7 +1085,7 @@ HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, boo
     l.hit = take(4 * rows);
     l.sums = take(8 * ((rows + 7) / 8));
   } else {
-    const Cut c = cut_of(rows > 0 ? rows : 1, vocab, cols, bf16, twin);
+    const Cut c = cut_of(rows > 0 ? rows : 1, vocab, cols, bf16, rows > 0 && rows <= twin_rows ? 1 : 0);
     l.kind = c.shape->kind;
     l.width = c.width;
     l.splits = c.splits;

@@ -115,11 +115,11 @@ adapm_status_t head_args(const adapm_head_t* h, adapm_rows_t x, adapm_rows_t wei
   d.loss = d.row_loss = d.lse = nullptr;
   d.ws = (char*)const_cast<void*>(workspace);
   d.w_packed = !in_place(h, weight);
-  d.twin = backward ? head_twin(h->rows, d.bf16, row_weight != nullptr) : 0;
+  d.twin_rows = backward ? head_twin_rows(d.bf16, row_weight != nullptr) : 0;
   const bool as_it_is = in_place(h, x) && x.stride <= (1ll << 21);
   d.direct = !backward && head_direct(h->rows) && as_it_is;
   d.whole = head_whole(h->rows) && as_it_is;
-  d.lay = head_layout(h->rows, h->vocab, h->cols, d.bf16, d.w_packed, backward, want_dx, d.twin);
+  d.lay = head_layout(h->rows, h->vocab, h->cols, d.bf16, d.w_packed, backward, want_dx, d.twin_rows);
   if (d.lay.threads >= GRID_THREADS) return fail(ADAPM_EINVAL, "rows %lld x vocab %lld: too many for one call", (long long)h->rows, (long long)h->vocab);
   if (h->rows && workspace_bytes < (size_t)d.lay.bytes)
     return fail(ADAPM_EINVAL, "workspace of %zu bytes, %lld are needed", workspace_bytes, (long long)d.lay.bytes);
@@ -230,7 +230,7 @@ size_t adapm_head_workspace_bytes(const adapm_head_t* h, adapm_rows_t weight, in
   const bool bf16 = h->dtype == ADAPM_BF16, packed = !in_place(h, weight);
   int64_t bytes = 0;
   for (int weighted = 0; weighted < (backward ? 2 : 1); ++weighted) {
-    const HeadLayout l = head_layout(h->rows, h->vocab, h->cols, bf16, packed, backward != 0, true, backward ? head_twin(h->rows, bf16, weighted != 0) : 0);
+    const HeadLayout l = head_layout(h->rows, h->vocab, h->cols, bf16, packed, backward != 0, true, backward ? head_twin_rows(bf16, weighted != 0) : 0);
     if (l.threads >= GRID_THREADS) return 0;
     bytes = l.bytes > bytes ? l.bytes : bytes;
   }

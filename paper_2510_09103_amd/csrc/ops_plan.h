@@ -54,6 +54,7 @@ struct HeadLayout {
   int64_t part, hit, sums;                                    // forward: maxima and sums of the tiles, target logits, loss sums
   int tiles;                                                  // ... of which each row has so many
   int64_t p, acc;                                             // backward: a piece of P, sums of dx
+  int64_t p_rows;                                             // ... rows of P, of packed x and of a part of dx that there is space for
   int64_t width;                                              // ... vocabulary rows of a piece
   int splits;                                                 // ... parts of dx's contraction over them
   bool dx_first;                                              // ... dx's tiles are given out before dW's
@@ -76,11 +77,11 @@ struct HeadDev {
   int w_packed;
   int direct;                    // forward: x is read where it is
   int whole;                     // x is read where it is if all of its rows count
-  int twin;                      // backward: P as two numbers
+  int twin_rows;                 // backward: P as two numbers if no more rows count
 };
 
-// backward: 1 if P of so many rows is kept as two numbers
-int head_twin(int64_t rows, bool bf16, bool weighted);
+// backward: up to how many rows that count P is kept as two numbers
+int head_twin_rows(bool bf16, bool weighted);
 
 // whether a forward pass of so many rows reads x where it is, if x's rows are whole aligned vectors
 bool head_direct(int64_t rows);
@@ -88,7 +89,7 @@ bool head_direct(int64_t rows);
 bool head_whole(int64_t rows);
 
 // backward: whether space for the gradients' pass is wanted (else the forward pass)
-HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx, int twin);
+HeadLayout head_layout(int64_t rows, int64_t vocab, int64_t cols, bool bf16, bool w_packed, bool backward, bool want_dx, int twin_rows);
 void launch_head_loss(const HeadDev& h, hipStream_t s);
 void launch_head_backward(const HeadDev& h, hipStream_t s);
 

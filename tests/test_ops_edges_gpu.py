@@ -42,6 +42,68 @@ def test_sure_rows_keep_the_digits_of_their_loss(rows, vocab, dtype):
     R.within("lse", r.lse.cpu(), torch.tensor([top for top, _ in pairs], dtype=torch.float64)[i] + want, off)
 
 
+def gradients(x, W, t, weight):
+    """The gradients' errors against 64 bits over those of their rounding to bf16, which no result can be below."""
+    r = ops.head_loss(x, W, t, row_weight=weight)
+    want = R.head(x, W, t, row_weight=weight)
+    worst = 0.0
+    for name, got in zip(("dx", "dw"), ops.head_backward(x, W, t, r.lse, row_weight=weight)):
+        worst = max(worst, float((got.double() - want[name]).norm() / (want[name].to(BF16).double() - want[name]).norm()))
+    return worst
+
+
+def some_rows_count(rows, live, weighted, vocab=1500, cols=160):
+    g = torch.Generator("cuda").manual_seed(rows + live)
+    W = (torch.randn(vocab, cols, device="cuda", generator=g) * (1.5 / cols ** 0.5)).to(BF16)
+    t = torch.full((rows,), -100, device="cuda")
+    at = torch.randperm(rows, device="cuda", generator=g)[:live]
+    t[at] = torch.randint(0, vocab, (live,), device="cuda", generator=g)
+    x = torch.randn(rows, cols, device="cuda", generator=g).to(BF16)
+    return x, W, t, torch.randn(rows, device="cuda", generator=g) if weighted else None
+
+
+@pytest.mark.parametrize("rows,live,weighted", [(4096, 16, False), (33, 32, False), (300, 1, False), (1025, 32, False), (2000, 50, True), (1300, 1024, True),
+                                                (1025, 1000, True), (5000, 1, True), (1026, 0, True)])
+def test_few_rows_that_count_keep_the_precision_of_the_type(rows, live, weighted):
+    """How many rows count decides whether P is kept as two numbers, not how many there are: 2^-17 / 1.7e-3 = 0.5 % and the fp32 sums beside it."""
+    x, W, t, weight = some_rows_count(rows, live, weighted)
+    if live:
+        assert gradients(x, W, t, weight) < 1.02
+    # one gradient alone, and a replay with another number of rows that count
+    r = ops.head_loss(x, W, t, row_weight=weight)
+    dx, dW = ops.head_backward(x, W, t, r.lse, row_weight=weight)
+    assert torch.equal(ops.head_backward(x, W, t, r.lse, row_weight=weight, need_dweight=False)[0], dx)
+    assert torch.equal(ops.head_backward(x, W, t, r.lse, row_weight=weight, need_dx=False)[1], dW)
+    assert not bool(dx[t < 0].any()) and (live or not bool(dW.any()))
+
+
+@pytest.mark.parametrize("rows,live,weighted", [(33, 33, False), (2100, 40, False), (2100, 2100, False), (1025, 1025, True), (3000, 1500, True)])
+def test_more_rows_that_count_lose_one_rounding_of_p(rows, live, weighted):
+    """P as one bf16 number: independent of the gradients' own rounding and, where one element of P makes the gradient, as large: 2^0.5.  The
+    mean square of the relative error of so many rows (weights: a third of them) is off by its own spread, 0.9 / n^0.5, five times that at most."""
+    n = live / 3 if weighted else live
+    assert gradients(*some_rows_count(rows, live, weighted)) < (2 + 5 * 0.9 / n ** 0.5) ** 0.5
+
+
+def test_replays_while_few_and_many_rows_count():
+    x, W, t, weight = some_rows_count(2000, 2000, True)
+    keep = t.clone()
+    ops.head_backward(x, W, t, ops.head_loss(x, W, t, row_weight=weight).lse, row_weight=weight)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = ops.head_loss(x, W, t, row_weight=weight)
+        dx, dW = ops.head_backward(x, W, t, r.lse, row_weight=weight)
+    for out in (1900, 0, 975, 976, 977, 2000, 1000):
+        t.copy_(keep)
+        t[:out] = -100
+        graph.replay()
+        torch.cuda.synchronize()
+        want = ops.head_loss(x, W, t, row_weight=weight)
+        for a, b in zip((*r, dx, dW), (*want, *ops.head_backward(x, W, t, want.lse, row_weight=weight))):
+            assert torch.equal(a, b), out
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,out", [(6, 3), (40, 11), (1300, 500), (20, 20), (1300, 1300)])
 @pytest.mark.parametrize("factor", [float("inf"), float("nan"), 3e38])

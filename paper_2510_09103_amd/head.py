@@ -24,7 +24,8 @@ class HeadStep(NamedTuple):
 
 
 class LMHead:
-    """blocks: the table.  p, seed: dropout on x before it is added (GPT-2 runs); every step draws from the counter (seed, t)."""
+    """blocks: the table.  p, seed: dropout on x before it is added (GPT-2 runs); every step draws from the counter (seed, t), or
+    (seed, t + offset_dev) where a captured step reads its counter on the device."""
 
     def __init__(self, blocks: Sequence[BlockSpec], eps: float = 1e-5, p: float = 0.0, seed: int = 0x5EED):
         self.norm = self._find(blocks, NORM_NAMES, "final norm")
@@ -44,11 +45,14 @@ class LMHead:
         raise ValueError(f"the table has no {what} (a block named {', '.join(names)})")
 
     def step(self, params: List[torch.Tensor], grads: List[torch.Tensor], x: torch.Tensor, residual: Optional[torch.Tensor],
-             targets: torch.Tensor, t: int, row_weight: Optional[torch.Tensor] = None, scale: float = 1.0) -> HeadStep:
+             targets: torch.Tensor, t: int, row_weight: Optional[torch.Tensor] = None, scale: float = 1.0,
+             offset_dev: Optional[torch.Tensor] = None) -> HeadStep:
         """Forward and backward pass of step t (1-based) on a batch of hidden states (any leading dimensions, the type of the table's
         gradients).  Overwrites grads[norm] and grads[head]; where the head is the embedding, what the embedding's look-up adds to
-        that gradient is the caller's to add afterwards.  Parameters of another type (fp32 masters of a bf16 model) are cast first."""
-        rng = ops.Rng(self.seed, t)
+        that gradient is the caller's to add afterwards.  Parameters of another type (fp32 masters of a bf16 model) are cast first.
+        A captured step holds t for ever: with p > 0 give it offset_dev, an int64 tensor of one element that is added to t on the device,
+        and set that before every replay; without it all replays have one mask."""
+        rng = ops.Rng(self.seed, t, offset_dev)
         weight, gain = params[self.head], params[self.norm]
         if weight.dtype != x.dtype:
             weight = weight.to(x.dtype)

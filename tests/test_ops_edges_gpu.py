@@ -144,3 +144,38 @@ def test_8_bit_rows_near_nothing(cols, dtype):
         off = 2.0 ** -4 * y.abs() + 2.0 ** -10 * scale + 60 * R.U * (y.abs() + scale) + 2.0 ** -149
         if top > 2.0 ** -150:
             assert bool(((got - y).abs() <= off).all()), (i, float(((got - y).abs() - off).max()))
+
+
+# ---- over a table -------------------------------------------------------------------------------------------------------
+
+def test_a_captured_end_of_a_model_draws_new_masks():
+    """Replays of LMHead.step whose counter on the device moves on are the eager steps of those numbers."""
+    from dataclasses import replace
+    from paper_2510_09103_amd import workloads as WL
+    from paper_2510_09103_amd.head import LMHead
+    wl = WL.gpt2_350m()
+    wl = replace(wl, blocks=tuple(replace(b, rows=600) if b.name == "wte" else b for b in wl.blocks if b.name in ("wte", "ln_f")))
+    x, res, t = WL.head_batch(wl, 150, device="cuda")
+    params = WL.initial_params(wl, device="cuda")
+    grads = [torch.zeros_like(p) for p in params]
+    end = LMHead(wl.blocks, p=0.2)
+    counter = torch.zeros(1, dtype=torch.int64, device="cuda")
+    end.step(params, grads, x, res, t, 0, offset_dev=counter)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = end.step(params, grads, x, res, t, 0, offset_dev=counter)
+    masks = []
+    for step in (1, 2, 3):
+        counter.fill_(step)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [g.clone() for g in (*out, *grads)]
+        want = end.step(params, grads, x, res, t, step)
+        assert all(torch.equal(a, b) for a, b in zip(got, (*want, *grads))), step
+        masks.append(got[2] == 0)
+    dropped = torch.stack(masks).double().mean().item()
+    assert abs(dropped - 0.2) < 5 * (0.16 / (3 * x.numel())) ** 0.5 + 1e-3            # exact zeros that were not dropped: few
+    for a, b in ((0, 1), (1, 2), (0, 2)):
+        both = (masks[a] & masks[b]).double().mean().item()
+        assert abs(both - 0.04) < 5 * (0.04 * 0.96 / x.numel()) ** 0.5 + 1e-3

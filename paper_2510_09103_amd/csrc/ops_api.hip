@@ -43,6 +43,7 @@ adapm_status_t drop_of(const adapm_dropout_t* d, int64_t rows, int64_t cols, Dro
   *out = DropDev{0, 0, 0, nullptr, 0, 1.f};
   if (!d) return ADAPM_OK;
   if (!(d->p >= 0.f && d->p < 1.f)) return fail(ADAPM_EINVAL, "dropout probability %g not in [0, 1)", (double)d->p);
+  if (d->reserved) return fail(ADAPM_EINVAL, "dropout: reserved is %d, 0 is wanted", d->reserved);
   if ((uintptr_t)d->offset_dev & 7) return fail(ADAPM_EINVAL, "offset_dev is not 8-byte aligned");
   if (rows > (1ll << 32) || cols > (1ll << 34)) return fail(ADAPM_EINVAL, "dropout: too many rows or columns for its counter");
   // 16 random bits decide: the probability is the nearest multiple of 2^-16, and the scale is that probability's
@@ -63,6 +64,7 @@ adapm_status_t check_norm(const adapm_norm_t* n) {
   if (n->rows < 0 || n->rows > (1ll << 31)) return fail(ADAPM_EINVAL, "rows %lld out of range", (long long)n->rows);
   if (n->cols < 1 || n->cols > NORM_COLS) return fail(ADAPM_EINVAL, "cols %lld not in [1, %lld]", (long long)n->cols, (long long)NORM_COLS);
   if (!is_float(n->dtype) || !is_float(n->weight_dtype)) return fail(ADAPM_EINVAL, "unknown dtype");
+  if (n->reserved) return fail(ADAPM_EINVAL, "norm: reserved is %d, 0 is wanted", n->reserved);
   if (!(n->eps >= 0.f) || !std::isfinite(n->eps)) return fail(ADAPM_EINVAL, "eps must be finite and >= 0");
   return ADAPM_OK;
 }
@@ -74,6 +76,7 @@ adapm_status_t check_head(const adapm_head_t* h) {
   if (h->cols < 1 || h->cols > (1ll << 16)) return fail(ADAPM_EINVAL, "cols %lld not in [1, 2^16]", (long long)h->cols);
   if (!is_float(h->dtype)) return fail(ADAPM_EINVAL, "unknown dtype %d", h->dtype);
   if (h->reduction != ADAPM_REDUCE_SUM && h->reduction != ADAPM_REDUCE_MEAN) return fail(ADAPM_EINVAL, "unknown reduction %d", h->reduction);
+  if (h->reserved) return fail(ADAPM_EINVAL, "head: reserved is %d, 0 is wanted", h->reserved);
   if (!std::isfinite(h->scale)) return fail(ADAPM_EINVAL, "scale is not finite");
   return ADAPM_OK;
 }

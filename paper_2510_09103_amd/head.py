@@ -10,10 +10,7 @@ from typing import List, NamedTuple, Optional, Sequence
 import torch
 
 from . import ops
-from .workloads import BlockSpec
-
-NORM_NAMES = ("ln_f", "norm_f")              # final norm vector
-HEAD_NAMES = ("lm_head", "wte", "embed")     # output head; the embedding where the table ties them
+from .workloads import HEAD_NAMES, NORM_NAMES, BlockSpec, find_block
 
 
 class HeadStep(NamedTuple):
@@ -28,21 +25,13 @@ class LMHead:
     (seed, t + offset_dev) where a captured step reads its counter on the device."""
 
     def __init__(self, blocks: Sequence[BlockSpec], eps: float = 1e-5, p: float = 0.0, seed: int = 0x5EED):
-        self.norm = self._find(blocks, NORM_NAMES, "final norm")
-        self.head = self._find(blocks, HEAD_NAMES, "output head")
+        self.norm = find_block(blocks, NORM_NAMES, "final norm")
+        self.head = find_block(blocks, HEAD_NAMES, "output head")
         n, h = blocks[self.norm], blocks[self.head]
         if n.numel != h.cols:
             raise ValueError(f"block {n.name} has {n.numel} elements, {h.name} {h.cols} columns")
         self.blocks, self.eps, self.p, self.seed = list(blocks), eps, p, seed
         self.tied = h.name != "lm_head"
-
-    @staticmethod
-    def _find(blocks, names, what):
-        for name in names:
-            for i, b in enumerate(blocks):
-                if b.name == name:
-                    return i
-        raise ValueError(f"the table has no {what} (a block named {', '.join(names)})")
 
     def step(self, params: List[torch.Tensor], grads: List[torch.Tensor], x: torch.Tensor, residual: Optional[torch.Tensor],
              targets: torch.Tensor, t: int, row_weight: Optional[torch.Tensor] = None, scale: float = 1.0,

@@ -281,10 +281,23 @@ class GradientStream:
         return out
 
 
+NORM_NAMES = ("ln_f", "norm_f")              # final norm vector of a table
+HEAD_NAMES = ("lm_head", "wte", "embed")     # its output head; the embedding where the table ties them
+
+
+def find_block(blocks, names, what: str) -> int:
+    """Place of the block with the first of the names that the table has."""
+    for name in names:
+        for i, b in enumerate(blocks):
+            if b.name == name:
+                return i
+    raise ValueError(f"the table has no {what} (a block named {', '.join(names)})")
+
+
 def head_batch(wl: Workload, tokens: int, masked: float = 0.0, seed: int = 0, device="cpu"):
     """(x, residual, targets) of a synthetic batch for the end of a model over wl's table (LMHead): what the last layer adds and the
     residual stream in the table's gradient type, and Zipf-distributed targets of which a share `masked` carries none (-100)."""
-    head = next(b for name in ("lm_head", "wte", "embed") for b in wl.blocks if b.name == name)
+    head = wl.blocks[find_block(wl.blocks, HEAD_NAMES, "output head")]
     g = _gen(device, wl.seed, seed, 4)
     dt = _TORCH_DT[head.grad_dtype]
     x = torch.randn(tokens, head.cols, device=device, generator=g).to(dt)

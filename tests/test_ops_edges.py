@@ -25,3 +25,9 @@ def test_reserved_fields_are_zero(call):
 def test_descriptors_with_reserved_fields_need_no_workspace():
     assert B.adapm_norm_workspace_bytes(B.adapm_norm_t(4, 64, 1, 0, 1, 0, 1e-5, 7)) == 0
     assert B.adapm_head_workspace_bytes(B.adapm_head_t(4, 100, 64, 1, 1, 1.0, 7), ROWS, 1) == 0
+
+
+def test_a_table_without_a_head_has_no_batch_for_one():
+    from paper_2510_09103_amd import workloads as WL
+    with pytest.raises(ValueError, match="output head"):
+        WL.head_batch(WL.tiny_block(), 4)

@@ -95,7 +95,7 @@ def main():
     ap.add_argument("--grad-clip", type=float, default=0.0, help="global gradient-norm clipping threshold (0 = off)")
     ap.add_argument("--rank", type=int, default=0, help="override the rank of every low-rank block (rank / T sweeps)")
     ap.add_argument("--head-tokens", type=int, default=0,
-                    help="also run the end of the model (residual norm, loss over the vocabulary, gradients of the norm and head "
+                    help="also run the end of the model (residual RMS norm, loss over the vocabulary, gradients of the norm and head "
                          "blocks) on a batch of that many tokens in front of the steps, and report it (0 = off)")
     ap.add_argument("--head-dropout", type=float, default=0.1, help="residual dropout of --head-tokens")
     args = ap.parse_args()
@@ -275,7 +275,7 @@ def main():
         products = 8.0 * args.head_tokens * b.numel      # logits, logits again, two gradients
         return {"tokens": args.head_tokens, "head": [b.rows, b.cols], "dropout": args.head_dropout, "loss": loss.item(), "ms_per_pass": ms,
                 "TFLOPs": products / (ms * 1e-3) / 1e12, "mfma_frac": products / (ms * 1e-3) / 1e12 / MFMA_BF16_PEAK_TFLOPS,
-                "note": "not part of ms_per_step; the gradients of the norm and head blocks that the timed steps read come from it"}
+                "note": "RMS norm also where the model has a LayerNorm; not part of ms_per_step; the gradients of the norm and head blocks that the timed steps read come from it"}
 
     model_end = head_bench() if args.head_tokens > 0 else None
     opt = make(args.T)

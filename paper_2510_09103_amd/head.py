@@ -1,7 +1,10 @@
 """The end of a model over a block table: residual dropout and addition, final norm, output head and loss, and their gradients written
 into the gradient tensors of the table's blocks, where AdaPM.step reads them.
 
-    h = residual + dropout(x);  y = norm(h) * params[norm];  loss = cross entropy of y params[head]^T
+    h = residual + dropout(x);  y = h / sqrt(mean(h^2) + eps) * params[norm];  loss = cross entropy of y params[head]^T
+
+The norm is the root-mean-square norm, whatever the table calls its vector.  A model whose final norm is a LayerNorm (GPT-2, blocks named
+ln_f: the mean is taken out first, and there is a bias) has other gradients than those made here; its tables stand for shapes.
 """
 from __future__ import annotations
 
@@ -21,7 +24,7 @@ class HeadStep(NamedTuple):
 
 
 class LMHead:
-    """blocks: the table.  p, seed: dropout on x before it is added (GPT-2 runs); every step draws from the counter (seed, t), or
+    """blocks: the table, whose norm block is taken for an RMS norm.  p, seed: dropout on x before it is added (GPT-2 runs); every step draws from the counter (seed, t), or
     (seed, t + offset_dev) where a captured step reads its counter on the device."""
 
     def __init__(self, blocks: Sequence[BlockSpec], eps: float = 1e-5, p: float = 0.0, seed: int = 0x5EED):
@@ -37,7 +40,7 @@ class LMHead:
              targets: torch.Tensor, t: int, row_weight: Optional[torch.Tensor] = None, scale: float = 1.0,
              offset_dev: Optional[torch.Tensor] = None) -> HeadStep:
         """Forward and backward pass of step t (1-based) on a batch of hidden states (any leading dimensions, the type of the table's
-        gradients).  Overwrites grads[norm] and grads[head]; where the head is the embedding, what the embedding's look-up adds to
+        gradients).  Overwrites grads[norm] and grads[head] (micro-batches are added up by the caller, in buffers of their own); where the head is the embedding, what the embedding's look-up adds to
         that gradient is the caller's to add afterwards.  Parameters of another type (fp32 masters of a bf16 model) are cast first.
         A captured step holds t for ever: with p > 0 give it offset_dev, an int64 tensor of one element that is added to t on the device,
         and set that before every replay; without it all replays have one mask."""

@@ -40,12 +40,13 @@ class LMHead:
              targets: torch.Tensor, t: int, row_weight: Optional[torch.Tensor] = None, scale: float = 1.0,
              offset_dev: Optional[torch.Tensor] = None) -> HeadStep:
         """Forward and backward pass of step t (1-based) on a batch of hidden states (any leading dimensions, the type of the table's
-        gradients).  Overwrites grads[norm] and grads[head] (micro-batches are added up by the caller, in buffers of their own); where the head is the embedding, what the embedding's look-up adds to
+        gradients).  Overwrites grads[norm] and grads[head] (micro-batches are added up by the caller, in buffers of their own) and leaves
+        no autograd graph; where the head is the embedding, what the embedding's look-up adds to
         that gradient is the caller's to add afterwards.  Parameters of another type (fp32 masters of a bf16 model) are cast first.
         A captured step holds t for ever: with p > 0 give it offset_dev, an int64 tensor of one element that is added to t on the device,
         and set that before every replay; without it all replays have one mask."""
         rng = ops.Rng(self.seed, t, offset_dev)
-        weight, gain = params[self.head], params[self.norm]
+        weight, gain = params[self.head].detach(), params[self.norm].detach()
         if weight.dtype != x.dtype:
             weight = weight.to(x.dtype)
         n = ops.rms_norm(x, gain, eps=self.eps, residual=residual, p=self.p, rng=rng)

@@ -3,8 +3,9 @@ over the vocabulary, each with its gradient.  All arithmetic happens in libadapm
 outputs and scratch from PyTorch on the current stream of the tensors' device, and make one library call (head_loss: the call of
 the forward pass).
 
-There is no autograd here: a training step calls the forward and the backward functions itself, as it calls AdaPM.step, and hands
-the gradients on in the buffers it likes (`out` / `dx` / `dweight` arguments).
+There is no autograd here: tensors that require gradients (parameters) are taken as data, and what a function returns or writes has no graph.
+A training step calls the forward and the backward functions itself, as it calls AdaPM.step, and hands the gradients on in the buffers it
+likes (`out` / `dx` / `dweight` arguments).
 """
 from __future__ import annotations
 
@@ -154,7 +155,8 @@ def _scratch(nbytes, like):
 
 def dropout(x: torch.Tensor, p: float, rng: Rng, residual: Optional[torch.Tensor] = None,
             out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """residual + dropout(x), rounded once.  The gradient of x is dropout(gradient of the result, p, rng).  out may be x or residual."""
+    """residual + dropout(x), rounded once.  The gradient of x is dropout(gradient of the result, p, rng), which the
+    caller calls: the result has no autograd graph.  out may be x or residual."""
     dt = _float_type("x", x)
     xr, n, cols = _first("x", x)
     res = _NO_ROWS if residual is None else _rows("residual", residual, x, x.dtype, x.shape)
@@ -171,7 +173,8 @@ def dropout(x: torch.Tensor, p: float, rng: Rng, residual: Optional[torch.Tensor
 def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual: Optional[torch.Tensor] = None, p: float = 0.0,
              rng: Optional[Rng] = None, out_dtype: Optional[torch.dtype] = None) -> Norm:
     """h = residual + dropout(x), y = h / sqrt(mean(h^2) + eps) * weight over the last dimension.  out_dtype: that of x, or
-    torch.float8_e4m3fn with a scale for each row (y stands for y * scale)."""
+    torch.float8_e4m3fn with a scale for each row (y stands for y * scale).  The results have no autograd graph: the gradients are
+    rms_norm_backward's."""
     dt, wt = _float_type("x", x), _float_type("weight", weight)
     xr, n, cols = _first("x", x)
     w = _vector("weight", weight, cols, x, weight.dtype)
@@ -236,7 +239,8 @@ def _head(x, weight, targets, row_weight, reduction, scale):
 def head_loss(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, row_weight: Optional[torch.Tensor] = None,
               reduction: str = "mean", scale: float = 1.0) -> Loss:
     """Softmax cross entropy of x @ weight.T against targets (int64, one a row); rows whose target is outside the vocabulary (-100, say)
-    do not count.  loss = scale * sum(row_weight * row_loss), divided by the number of rows that count where reduction is "mean"."""
+    do not count.  loss = scale * sum(row_weight * row_loss), divided by the number of rows that count where reduction is "mean".  The
+    results have no autograd graph: the gradients are head_backward's."""
     h, xr, w, t, rw = _head(x, weight, targets, row_weight, reduction, scale)
     loss = x.new_empty((), dtype=torch.float32)
     row_loss = _empty(targets, torch.float32)

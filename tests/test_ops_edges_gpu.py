@@ -179,3 +179,22 @@ def test_a_captured_end_of_a_model_draws_new_masks():
     for a, b in ((0, 1), (1, 2), (0, 2)):
         both = (masks[a] & masks[b]).double().mean().item()
         assert abs(both - 0.04) < 5 * (0.04 * 0.96 / x.numel()) ** 0.5 + 1e-3
+
+
+def test_parameters_are_taken_as_data():
+    """Tensors that require gradients give the same bits as others, and nothing that is returned or written has a graph."""
+    from dataclasses import replace
+    from paper_2510_09103_amd import workloads as WL
+    from paper_2510_09103_amd.head import LMHead
+    wl = WL.llama_60m()
+    wl = replace(wl, blocks=tuple(replace(b, rows=500) if b.name == "embed" else b for b in wl.blocks if b.name in ("embed", "norm_f")))
+    x, res, t = WL.head_batch(wl, 90, device="cuda")
+    params = WL.initial_params(wl, device="cuda")
+    runs = []
+    for wanted in (False, True):
+        grads = [torch.zeros(b.rows, b.cols, dtype=BF16, device="cuda") for b in wl.blocks]
+        leaves = [p.clone().requires_grad_(wanted) for p in params]
+        out = LMHead(wl.blocks, p=0.1).step(leaves, grads, x.clone().requires_grad_(wanted), res.clone().requires_grad_(wanted), t, 1)
+        assert not any(g.requires_grad for g in (*out, *grads)) and all(p.grad is None for p in leaves)
+        runs.append([*out, *grads])
+    assert all(torch.equal(a, b) for a, b in zip(*runs))

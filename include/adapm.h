@@ -256,6 +256,8 @@ typedef struct {
 
 /* h = residual + dropout(x) in dtype, rstd = 1 / sqrt(mean(h^2) + eps) (fp32, one a row), y = h * rstd * weight.
  * residual.data and drop may be NULL; with neither, h.data may be NULL and the h of the backward pass is x itself.
+ * The squares and their sum are fp32: |h| up to 1e17 is in range in rows of any length (a sum past 3.4e38 gives rstd = 0, y = 0), and
+ * with eps = 0 rows whose largest value is 1e-16 or more (a row of zeros is NaN then).
  * y_dtype = ADAPM_E4M3: y holds 8-bit values and y_scale[row] = max|row| / 448 (1 for a row of zeros, at least 2^-126 for any
  * other; NaN does not count) is what they are multiplied by.  h may be x or residual; y overlaps none of the others. */
 adapm_status_t adapm_norm_forward(const adapm_norm_t* n, adapm_rows_t x, adapm_rows_t residual, adapm_rows_t h,

@@ -146,6 +146,18 @@ def test_8_bit_rows_near_nothing(cols, dtype):
             assert bool(((got - y).abs() <= off).all()), (i, float(((got - y).abs() - off).max()))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_norm_in_the_range_that_is_named(dtype):
+    """Values of 1e17 in the widest row, and of 1e-16 without eps: squares and their sum stay fp32 numbers."""
+    w = torch.ones(16384, device="cuda")
+    for size, eps in ((1e17, 1e-5), (1e-16, 0.0)):
+        x = (randn(2, 16384, seed=3).clamp(-1, 1) * size).to(dtype)
+        n = ops.rms_norm(x, w, eps=eps)
+        y, rstd = R.norm(x, w, eps)
+        R.within("rstd", n.rstd, rstd, 42 * R.U * rstd)
+        R.within("y", n.y, y, 46 * R.U * y.abs(), dtype)
+
+
 # ---- over a table -------------------------------------------------------------------------------------------------------
 
 def test_a_captured_end_of_a_model_draws_new_masks():

@@ -671,6 +671,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void piece_k
   product<C, true, true>(vocab_rows<T>(h, first, width), packed_x<T>(h, n), m0, n0, 0, h.cols, lds, acc);
   HEAD_LANE
   T* P = reinterpret_cast<T*>(h.ws + h.lay.p);
+  const bool two = uniform(twin(h, n));
 #pragma unroll
   for (int j = 0; j < C::NT; ++j) {
     const int row = n0 + un + 16 * j + l16;
@@ -711,7 +712,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void piece_k
 #pragma unroll
           for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(p[i + e / 2][2 * (e & 1)], p[i + e / 2][2 * (e & 1) + 1]);
           *reinterpret_cast<u32x4*>(to) = w;
-          if (twin(h, n)) {
+          if (two) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               w[e] = pack_bf16x2(p[i + e / 2][2 * (e & 1)] - bf16lo(w[e]), p[i + e / 2][2 * (e & 1) + 1] - bf16hi(w[e]));

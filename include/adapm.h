@@ -287,7 +287,8 @@ typedef struct {
 } adapm_head_t;
 
 /* Scratch of adapm_head_loss (backward = 0) or adapm_head_backward (1); 0 if h is invalid.  weight: as in the call (W whose rows
- * are not whole, 16-byte aligned vectors is copied there). */
+ * are not whole, 16-byte aligned vectors is copied there).  It has room for a packed copy of x, since the device alone knows whether all
+ * rows count and x can be read where it is. */
 size_t adapm_head_workspace_bytes(const adapm_head_t* h, adapm_rows_t weight, int32_t backward);
 
 /* targets[rows]: a row whose target lies outside [0, vocab) does not count: whatever it holds reaches nothing, its row_loss

@@ -8,7 +8,7 @@
 // logits and stored in the type of x (a piece is about PIECE_BYTES or 2048 vocabulary rows, not the rows x vocab of all logits), then one launch adds
 // its part to dx and writes its rows of dW.  The logits are made twice: to keep them in fp32
 // takes rows x vocab x 4 bytes, 1 GB for 8192 rows over 32000, which the operator is there to save.  For time alone it would depend on the columns: a
-// logit made again costs 2 cols flop, 0.8 ps of the matrix cores at 512 columns and 3.2 ps at 2048 (1270 TFLOP/s), one kept 8 bytes written and
+// logit made again costs 2 cols flop, 0.8 ps of the matrix cores at 512 columns and 3.3 ps at 2048 (1240 TFLOP/s), one kept 8 bytes written and
 // read, 1.6 ps of memory.  From about 1000 columns on chunks of rows whose logits stay small could be quicker, against a dW that
 // is added up in fp32 over the chunks; that is not built, and not measured.
 //
